@@ -294,6 +294,99 @@ int fsd_accept_labels(const float *divergence, int B, int positions, float thres
                       uint8_t *labels,             /* [B, positions] out */
                       void *stream);
 
+/* ---- Logit processing in front of a verify call ----
+ * Section 4 leaves the sampling method to the user ("with whatever sampling method the user sets").  These calls turn the
+ * logits of both models into those of the distributions that such a method samples from: penalties for tokens that were
+ * used, the caller's biases, a grammar's mask, a temperature, and top-k, top-p and min-p.  What a verify call is given has
+ * to have gone through the same on both sides, the draft's as its tokens were drawn.
+ *
+ * Row r of a sequence is conditioned on the tokens drafted before it (chain: the first r of them; tree: the node it stands
+ * after and its ancestors), and each of these counts as used in that row.  For token t of row r of sequence b:
+ *   n    = counts[b, t] + how often t is among the tokens drafted before the row
+ *   used = bit t of seen[b], or t is among those tokens
+ *   x    = the logit, widened to single precision
+ *   x    = used ? (x > 0 ? x * (1 / repetition[b]) : x * repetition[b]) : x
+ *   x    = x - frequency[b] * n,  then  x = x - presence[b] if n > 0
+ *   x    = x + bias of t
+ *   x    = -inf if bit t of the row's mask is 0, whatever the logit is
+ *   x    = x * (1 / temperature[b]) if temperature[b] > 0
+ *   y    = x, rounded to the logits' type
+ * in single precision, each operation (1 / repetition and 1 / temperature are two of them) rounded to nearest by itself.
+ * With any of top_k, top_p and min_p set, the row y is then cut off.  In the order of falling value, equal values by rising
+ * token id (-0 and 0 are equal):
+ *   top_k  keeps the first top_k[b] tokens (all if top_k[b] <= 0 or >= V)
+ *   top_p  keeps of these the ones whose predecessors have together less than the share top_p[b] of the top_k ones'
+ *          weight, exp(y), and the first one in any case (top_p[b] >= 1 or NaN: all)
+ *   min_p  keeps of these the ones whose weight is at least min_p[b] times the first one's (min_p[b] <= 0 or NaN: all;
+ *          above 1 it counts as 1)
+ * What is not kept becomes -inf.  Sums are in double precision.  A row that holds NaN, +inf or no finite value is not cut off
+ * (a verify call reports it). */
+typedef struct fsd_process_opts {
+    uint32_t struct_size;          /* sizeof(fsd_process_opts), for versioning */
+    int32_t  logit_dtype;          /* FSD_F32 | FSD_BF16, of all logit tensors of the call */
+    /* Device pointers; NULL leaves the step out. */
+    const int32_t  *counts;        /* [B, V]  how often each token has been generated, >= 0.  With `seen`, or both NULL. */
+    const uint32_t *seen;          /* [B, W]  W = ceil(V / 32); bit t % 32 of word t / 32: token t is in the prompt or has been
+                                      generated.  It has to be set where counts[b, t] > 0. */
+    const float *repetition;       /* [B] > 0.   counts, seen and the drafted tokens matter only where one of these three is set */
+    const float *frequency;        /* [B] finite */
+    const float *presence;         /* [B] finite */
+    const int32_t *bias_offsets;   /* [B + 1] sequence b's biases are entries bias_offsets[b] up to bias_offsets[b + 1] of */
+    const int32_t *bias_tokens;    /*   these two (all three or none are NULL); ids outside [0, V) count for nothing; of a */
+    const float   *bias_values;    /*   token that a sequence lists more than once the last entry counts */
+    const uint32_t *allowed;       /* [B, gamma + 1 or N + 1, W] a mask for each target row; a draft row uses that of the target
+                                      row with the same context (chain: row i; tree: row parent + 1) */
+    const float   *temperature;    /* [B] */
+    const int32_t *top_k;          /* [B] */
+    const float   *top_p;          /* [B] */
+    const float   *min_p;          /* [B] */
+} fsd_process_opts;
+
+/* Fills `opts` with the defaults: bf16 logits, every step left out.  Host pointer. */
+void fsd_default_process_opts(fsd_process_opts *opts);
+
+/* Chain rows.  gamma may be 0: one target row a sequence, for decoding token by token.
+ *   target_in, target_out [B, gamma+1, V]  row i stands after i drafted tokens.  The same pointer, or no memory in common.
+ *   draft_in,  draft_out  [B, gamma,   V]  or both NULL
+ *   draft_tokens [B, gamma] int32; NULL: drafted tokens do not count as used.  An id outside [0, V) counts for nothing.
+ *   opts         host pointer; the struct is read during the call, the arrays it points to when the kernels run
+ * The logits, masks and arrays as in the verify calls: row-major, contiguous, element-aligned; V at most 2^30.  The call needs no
+ * workspace, waits for nothing on the device and can be captured in a CUDA graph after one ordinary call on that device.
+ * Errors: FSD_ERR_NULL (a required pointer, or one of a group that goes together), FSD_ERR_SHAPE, FSD_ERR_ALIGN,
+ * FSD_ERR_ENUM, FSD_ERR_UNSUPPORTED (an output overlaps an input that it is not the same as, or another output), FSD_ERR_CUDA. */
+int fsd_process_chain(const void *target_in, const void *draft_in, const int32_t *draft_tokens,
+                      int B, int gamma, int V, const fsd_process_opts *opts,
+                      void *target_out, void *draft_out, void *stream);
+
+/* Tree rows, as in fsd_verify_tree: target row 0 after the root context, row j+1 after node j; draft row j is what node j's
+ * token was proposed from, so its context is that of target row parent[j] + 1.
+ *   parent      [B, N] int32  parent[j] in [-1, j); any other value counts as -1 here (a verify call reports it)
+ *   node_tokens [B, N] int32  or NULL: drafted tokens do not count as used
+ *   target_in, target_out [B, N+1, V];  draft_in, draft_out [B, N, V] or both NULL;  N at most 1024 */
+int fsd_process_tree(const void *target_in, const void *draft_in, const int32_t *parent, const int32_t *node_tokens,
+                     int B, int N, int V, const fsd_process_opts *opts,
+                     void *target_out, void *draft_out, void *stream);
+
+/* The counts and the bitmap that the penalties read, of B sequences, from nothing.  Sequence b's prompt is entries
+ * prompt_offsets[b] up to prompt_offsets[b + 1] of prompt_tokens, what it has generated so far is given in the same way
+ * (output_offsets and output_tokens both NULL: nothing).  Ids outside [0, V) count for nothing.
+ *   counts [B, V] out  how often each token is among the generated ones
+ *   seen   [B, W] out  a bit for each token that is in the prompt or among the generated ones; bits from V on are 0
+ * Offsets are [B + 1] int32 and >= 0; a sequence whose second is not above its first is empty.
+ * Errors: FSD_ERR_NULL, FSD_ERR_SHAPE, FSD_ERR_ALIGN, FSD_ERR_CUDA. */
+int fsd_history_build(const int32_t *prompt_offsets, const int32_t *prompt_tokens,
+                      const int32_t *output_offsets, const int32_t *output_tokens,
+                      int B, int V, int32_t *counts, uint32_t *seen, void *stream);
+
+/* What a verify call accepted joins them: the first accept_len[b] drafted tokens and next_token[b] (tree: the tokens of the
+ * first accept_len[b] nodes of path[b]).  accept_len is taken as at most gamma (max_depth) and at least 0; ids outside [0, V), -1 of
+ * a row without a valid distribution among them, and nodes outside [0, N) count for nothing. */
+int fsd_history_append_chain(const int32_t *draft_tokens, const int32_t *accept_len, const int32_t *next_token,
+                             int B, int gamma, int V, int32_t *counts, uint32_t *seen, void *stream);
+int fsd_history_append_tree(const int32_t *node_tokens, const int32_t *path, const int32_t *accept_len,
+                            const int32_t *next_token, int B, int N, int max_depth, int V,
+                            int32_t *counts, uint32_t *seen, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -41,6 +41,12 @@ class FsdOpts(C.Structure):
     ]
 
 
+class FsdProcessOpts(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("logit_dtype", C.c_int32)] + [
+        (name, C.c_void_p) for name in ("counts", "seen", "repetition", "frequency", "presence", "bias_offsets", "bias_tokens",
+                                        "bias_values", "allowed", "temperature", "top_k", "top_p", "min_p")]
+
+
 class FsdError(RuntimeError):
     def __init__(self, status: int):
         self.status = status
@@ -98,6 +104,18 @@ def _load():
         lib.fsd_calibrate_threshold.restype = C.c_int
         lib.fsd_accept_labels.argtypes = [vp, C.c_int, C.c_int, C.c_float, C.c_int, vp, C.c_void_p]
         lib.fsd_accept_labels.restype = C.c_int
+        lib.fsd_default_process_opts.argtypes = [C.POINTER(FsdProcessOpts)]
+        lib.fsd_default_process_opts.restype = None
+        lib.fsd_process_chain.argtypes = [vp, vp, ip, C.c_int, C.c_int, C.c_int, C.POINTER(FsdProcessOpts), vp, vp, vp]
+        lib.fsd_process_chain.restype = C.c_int
+        lib.fsd_process_tree.argtypes = [vp, vp, ip, ip, C.c_int, C.c_int, C.c_int, C.POINTER(FsdProcessOpts), vp, vp, vp]
+        lib.fsd_process_tree.restype = C.c_int
+        lib.fsd_history_build.argtypes = [ip, ip, ip, ip, C.c_int, C.c_int, ip, ip, vp]
+        lib.fsd_history_build.restype = C.c_int
+        lib.fsd_history_append_chain.argtypes = [ip, ip, ip, C.c_int, C.c_int, C.c_int, ip, ip, vp]
+        lib.fsd_history_append_chain.restype = C.c_int
+        lib.fsd_history_append_tree.argtypes = [ip, ip, ip, ip, C.c_int, C.c_int, C.c_int, C.c_int, ip, ip, vp]
+        lib.fsd_history_append_tree.restype = C.c_int
         _lib = lib
     return _lib
 
@@ -232,3 +250,54 @@ def fsd_calibrate_threshold(divergence, B, positions, target_mean_accept_len, co
 
 def fsd_accept_labels(divergence, B, positions, threshold, compare, labels, stream=None) -> int:
     return _load().fsd_accept_labels(_ptr(divergence), B, positions, float(threshold), compare, _ptr(labels), stream)
+
+
+def fsd_default_process_opts() -> FsdProcessOpts:
+    o = FsdProcessOpts()
+    _load().fsd_default_process_opts(C.byref(o))
+    return o
+
+
+def make_process_opts(dtype="bf16", **arrays) -> FsdProcessOpts:
+    """Options of the process calls.  `arrays`: device tensors (or integer addresses, or None) by the names of the struct's
+    fields.  The tensors are kept alive with the options; their types and layouts are those the C header gives, and are checked."""
+    o = fsd_default_process_opts()
+    o.logit_dtype = DTYPES[dtype]
+    whole = {"counts", "seen", "bias_offsets", "bias_tokens", "allowed", "top_k"}
+    known = {name for name, _ in FsdProcessOpts._fields_[2:]}
+    for name, t in arrays.items():
+        if name not in known:
+            raise TypeError(f"make_process_opts() got an unexpected option {name!r}")
+        if t is not None and not isinstance(t, int):
+            kind = str(t.dtype).replace("torch.", "")
+            if kind not in (("int32", "uint32") if name in whole else ("float32",)) or not t.is_contiguous():
+                raise ValueError(f"{name}: a contiguous {'int32' if name in whole else 'float32'} tensor is wanted, got {kind}"
+                                 f"{'' if t.is_contiguous() else ', not contiguous'}")
+        setattr(o, name, _ptr(t))
+    o._kept = dict(arrays)
+    return o
+
+
+def fsd_process_chain(target_in, draft_in, draft_tokens, B, gamma, V, opts, target_out, draft_out, stream=None) -> int:
+    return _load().fsd_process_chain(_ptr(target_in), _ptr(draft_in), _ptr(draft_tokens), B, gamma, V,
+                                     C.byref(opts) if opts is not None else None, _ptr(target_out), _ptr(draft_out), _ptr(stream))
+
+
+def fsd_process_tree(target_in, draft_in, parent, node_tokens, B, N, V, opts, target_out, draft_out, stream=None) -> int:
+    return _load().fsd_process_tree(_ptr(target_in), _ptr(draft_in), _ptr(parent), _ptr(node_tokens), B, N, V,
+                                    C.byref(opts) if opts is not None else None, _ptr(target_out), _ptr(draft_out), _ptr(stream))
+
+
+def fsd_history_build(prompt_offsets, prompt_tokens, output_offsets, output_tokens, B, V, counts, seen, stream=None) -> int:
+    return _load().fsd_history_build(_ptr(prompt_offsets), _ptr(prompt_tokens), _ptr(output_offsets), _ptr(output_tokens),
+                                     B, V, _ptr(counts), _ptr(seen), _ptr(stream))
+
+
+def fsd_history_append_chain(draft_tokens, accept_len, next_token, B, gamma, V, counts, seen, stream=None) -> int:
+    return _load().fsd_history_append_chain(_ptr(draft_tokens), _ptr(accept_len), _ptr(next_token), B, gamma, V,
+                                            _ptr(counts), _ptr(seen), _ptr(stream))
+
+
+def fsd_history_append_tree(node_tokens, path, accept_len, next_token, B, N, max_depth, V, counts, seen, stream=None) -> int:
+    return _load().fsd_history_append_tree(_ptr(node_tokens), _ptr(path), _ptr(accept_len), _ptr(next_token), B, N, max_depth, V,
+                                           _ptr(counts), _ptr(seen), _ptr(stream))

@@ -1,0 +1,168 @@
+// C ABI of the logit processing calls and of the token counts they read: argument checks and launches.
+// See include/fsd_verify.h for the contract of every entry point.
+#include <climits>
+#include <cstdint>
+#include <cuda_runtime.h>
+
+#include "fsd_verify.h"
+#include "fsd_device.cuh"
+#include "fsd_history.cuh"
+#include "fsd_process.cuh"
+#include "fsd_truncate.cuh"
+
+namespace {
+
+using namespace fsd;
+
+constexpr int kMaxV = 1 << 30;
+constexpr int kMaxNodes = 1024;        // as in the tree verification
+constexpr int kSMs = 148;
+
+inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return na != 0 && nb != 0 && x < y + nb && y < x + na;
+}
+inline int words(int V) { return (V + 31) / 32; }
+
+int check(const fsd_process_opts* o) {
+    if (o == nullptr) return FSD_ERR_NULL;
+    if (o->struct_size != sizeof(fsd_process_opts)) return FSD_ERR_ENUM;
+    if (o->logit_dtype < FSD_F32 || o->logit_dtype > FSD_BF16) return FSD_ERR_ENUM;
+    if ((o->counts == nullptr) != (o->seen == nullptr)) return FSD_ERR_NULL;
+    const int biases = (o->bias_offsets != nullptr) + (o->bias_tokens != nullptr) + (o->bias_values != nullptr);
+    if (biases != 0 && biases != 3) return FSD_ERR_NULL;
+    for (const void* p : {static_cast<const void*>(o->counts), static_cast<const void*>(o->seen), static_cast<const void*>(o->repetition),
+                          static_cast<const void*>(o->frequency), static_cast<const void*>(o->presence), static_cast<const void*>(o->bias_offsets),
+                          static_cast<const void*>(o->bias_tokens), static_cast<const void*>(o->bias_values), static_cast<const void*>(o->allowed),
+                          static_cast<const void*>(o->temperature), static_cast<const void*>(o->top_k), static_cast<const void*>(o->top_p),
+                          static_cast<const void*>(o->min_p)})
+        if (!aligned(p, 4)) return FSD_ERR_ALIGN;
+    return FSD_OK;
+}
+
+template <int DT>
+int launch(const ProcArgs& a, bool cut, cudaStream_t s) {
+    const int per_block = kProcThreads * Logit<DT>::kPerVec;
+    const int all = a.rows[0] + a.rows[1];
+    // a row's last vector may lie one further than its length says (see the kernel)
+    const long long spans = (a.V + Logit<DT>::kPerVec - 1 + per_block - 1) / per_block;
+    // as many rows a block as leave eight blocks an SM, so that the counts are read for many rows at once
+    long long group = spans * a.B * all / (8 * kSMs);
+    group = group < 1 ? 1 : group > all ? all : group;
+    const long long groups = (all + group - 1) / group;
+    if (spans * groups * a.B > INT_MAX) return FSD_ERR_SHAPE;
+    fsd_process_kernel<DT><<<static_cast<unsigned>(spans * groups * a.B), kProcThreads, 0, s>>>(a, static_cast<int>(spans), static_cast<int>(groups), static_cast<int>(group));
+    if (cudaGetLastError() != cudaSuccess) return FSD_ERR_CUDA;
+    if (cut) {
+        fsd_truncate_kernel<DT><<<static_cast<unsigned>(a.B) * all, kCutThreads, 0, s>>>(a);
+        if (cudaGetLastError() != cudaSuccess) return FSD_ERR_CUDA;
+    }
+    return FSD_OK;
+}
+
+int process(const void* target_in, const void* draft_in, const int32_t* parent, const int32_t* tokens, int B, int P, int V,
+            const fsd_process_opts* o, void* target_out, void* draft_out, void* stream) {
+    if (target_in == nullptr || target_out == nullptr || (draft_in == nullptr) != (draft_out == nullptr)) return FSD_ERR_NULL;
+    if (B < 1 || V < 1 || V > kMaxV || static_cast<long long>(B) * (2ll * P + 1) > INT_MAX) return FSD_ERR_SHAPE;
+    const size_t es = o->logit_dtype == FSD_BF16 ? 2 : 4;
+    if (!aligned(target_in, es) || !aligned(target_out, es) || !aligned(draft_in, es) || !aligned(draft_out, es) || !aligned(parent, 4) || !aligned(tokens, 4))
+        return FSD_ERR_ALIGN;
+    const size_t W4 = static_cast<size_t>(words(V)) * 4, nB = static_cast<size_t>(B) * 4;
+    const size_t nt = static_cast<size_t>(B) * (P + 1) * V * es, nd = draft_in != nullptr ? static_cast<size_t>(B) * P * V * es : 0;
+    const struct { const void* p; size_t n; } ins[] = {
+        {target_in, nt}, {draft_in, nd}, {parent, nB * P}, {tokens, nB * P}, {o->counts, nB * V}, {o->seen, B * W4}, {o->repetition, nB}, {o->frequency, nB},
+        {o->presence, nB}, {o->bias_offsets, nB + 4}, {o->allowed, static_cast<size_t>(B) * (P + 1) * W4}, {o->temperature, nB}, {o->top_k, nB}, {o->top_p, nB},
+        {o->min_p, nB}};
+    for (const auto& in : ins) {
+        if (in.p == nullptr) continue;
+        if (overlap(in.p, in.n, target_out, nt) && !(in.p == target_in && target_in == target_out)) return FSD_ERR_UNSUPPORTED;
+        if (nd != 0 && overlap(in.p, in.n, draft_out, nd) && !(in.p == draft_in && draft_in == draft_out)) return FSD_ERR_UNSUPPORTED;
+    }
+    if (overlap(target_out, nt, draft_out, nd)) return FSD_ERR_UNSUPPORTED;
+    ProcArgs a = {};
+    a.in[0] = target_in; a.in[1] = draft_in;
+    a.out[0] = target_out; a.out[1] = draft_out;
+    a.rows[0] = P + 1; a.rows[1] = draft_in != nullptr ? P : 0;
+    a.tokens = P > 0 ? tokens : nullptr;
+    a.parent = parent;
+    a.B = B; a.P = P; a.V = V; a.W = words(V);
+    a.penalties = o->repetition != nullptr || o->frequency != nullptr || o->presence != nullptr;
+    a.repetition = o->repetition; a.frequency = o->frequency; a.presence = o->presence;
+    a.counts = o->counts; a.seen = o->seen;
+    a.bias_offsets = o->bias_offsets; a.bias_tokens = o->bias_tokens; a.bias_values = o->bias_values;
+    a.allowed = o->allowed; a.temperature = o->temperature;
+    a.top_k = o->top_k; a.top_p = o->top_p; a.min_p = o->min_p;
+    const bool cut = o->top_k != nullptr || o->top_p != nullptr || o->min_p != nullptr;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return o->logit_dtype == FSD_BF16 ? launch<FSD_BF16>(a, cut, s) : launch<FSD_F32>(a, cut, s);
+}
+
+int append(const int32_t* tokens, const int32_t* path, const int32_t* accept_len, const int32_t* next_token, int B, int P, int width, int V,
+           int32_t* counts, uint32_t* seen, void* stream) {
+    if (V > kMaxV || static_cast<long long>(B) * (P > width ? P : width) > INT_MAX) return FSD_ERR_SHAPE;
+    for (const void* p : {static_cast<const void*>(tokens), static_cast<const void*>(path), static_cast<const void*>(accept_len),
+                          static_cast<const void*>(next_token), static_cast<const void*>(counts), static_cast<const void*>(seen)})
+        if (!aligned(p, 4)) return FSD_ERR_ALIGN;
+    fsd_history_append_kernel<<<static_cast<unsigned>((B + 3) / 4), 128, 0, static_cast<cudaStream_t>(stream)>>>(tokens, path, accept_len, next_token, B, P, width, V,
+                                                                                                             words(V), counts, seen);
+    return cudaGetLastError() == cudaSuccess ? FSD_OK : FSD_ERR_CUDA;
+}
+
+}  // namespace
+
+extern "C" {
+
+void fsd_default_process_opts(fsd_process_opts* opts) {
+    if (opts == nullptr) return;
+    *opts = {};
+    opts->struct_size = sizeof(fsd_process_opts);
+    opts->logit_dtype = FSD_BF16;
+}
+
+int fsd_process_chain(const void* target_in, const void* draft_in, const int32_t* draft_tokens, int B, int gamma, int V,
+                      const fsd_process_opts* opts, void* target_out, void* draft_out, void* stream) {
+    const int rc = check(opts);
+    if (rc != FSD_OK) return rc;
+    if (gamma < 0) return FSD_ERR_SHAPE;
+    return process(target_in, draft_in, nullptr, draft_tokens, B, gamma, V, opts, target_out, draft_out, stream);
+}
+
+int fsd_process_tree(const void* target_in, const void* draft_in, const int32_t* parent, const int32_t* node_tokens, int B, int N, int V,
+                     const fsd_process_opts* opts, void* target_out, void* draft_out, void* stream) {
+    const int rc = check(opts);
+    if (rc != FSD_OK) return rc;
+    if (parent == nullptr) return FSD_ERR_NULL;
+    if (N < 1 || N > kMaxNodes) return FSD_ERR_SHAPE;
+    return process(target_in, draft_in, parent, node_tokens, B, N, V, opts, target_out, draft_out, stream);
+}
+
+int fsd_history_build(const int32_t* prompt_offsets, const int32_t* prompt_tokens, const int32_t* output_offsets, const int32_t* output_tokens,
+                      int B, int V, int32_t* counts, uint32_t* seen, void* stream) {
+    if (prompt_offsets == nullptr || prompt_tokens == nullptr || (output_offsets == nullptr) != (output_tokens == nullptr) || counts == nullptr || seen == nullptr)
+        return FSD_ERR_NULL;
+    const long long spans = (static_cast<long long>(V) + kHistSpan - 1) / kHistSpan;
+    if (B < 1 || V < 1 || V > kMaxV || spans * B > INT_MAX) return FSD_ERR_SHAPE;
+    for (const void* p : {static_cast<const void*>(prompt_offsets), static_cast<const void*>(prompt_tokens), static_cast<const void*>(output_offsets),
+                          static_cast<const void*>(output_tokens), static_cast<const void*>(counts), static_cast<const void*>(seen)})
+        if (!aligned(p, 4)) return FSD_ERR_ALIGN;
+    fsd_history_build_kernel<<<static_cast<unsigned>(spans * B), kHistThreads, 0, static_cast<cudaStream_t>(stream)>>>(
+        prompt_offsets, prompt_tokens, output_offsets, output_tokens, V, words(V), static_cast<int>(spans), counts, seen);
+    return cudaGetLastError() == cudaSuccess ? FSD_OK : FSD_ERR_CUDA;
+}
+
+int fsd_history_append_chain(const int32_t* draft_tokens, const int32_t* accept_len, const int32_t* next_token, int B, int gamma, int V,
+                             int32_t* counts, uint32_t* seen, void* stream) {
+    if (draft_tokens == nullptr || accept_len == nullptr || next_token == nullptr || counts == nullptr || seen == nullptr) return FSD_ERR_NULL;
+    if (B < 1 || gamma < 1 || V < 1) return FSD_ERR_SHAPE;
+    return append(draft_tokens, nullptr, accept_len, next_token, B, gamma, gamma, V, counts, seen, stream);
+}
+
+int fsd_history_append_tree(const int32_t* node_tokens, const int32_t* path, const int32_t* accept_len, const int32_t* next_token, int B, int N,
+                            int max_depth, int V, int32_t* counts, uint32_t* seen, void* stream) {
+    if (node_tokens == nullptr || path == nullptr || accept_len == nullptr || next_token == nullptr || counts == nullptr || seen == nullptr) return FSD_ERR_NULL;
+    if (B < 1 || N < 1 || max_depth < 1 || V < 1) return FSD_ERR_SHAPE;
+    return append(node_tokens, path, accept_len, next_token, B, N, max_depth, V, counts, seen, stream);
+}
+
+}  // extern "C"
