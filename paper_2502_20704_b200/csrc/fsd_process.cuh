@@ -185,9 +185,10 @@ __device__ __forceinline__ Used<N> load_used(const ProcArgs& a, int b, int t0) {
 }
 
 // The steps on one vector of a row.  special: which of its ids are in the span's bitmap; may: the row's mask.
-template <int DT, int SPAN>
-__device__ __forceinline__ void process_vec(const ProcArgs& a, const SeqParams& p, int b, int ctx, int t0, int lo, const Used<Logit<DT>::kPerVec>& u,
-                                            uint32_t special, uint32_t may, const Special<SPAN>& s, float (&x)[Logit<DT>::kPerVec]) {
+// bias_of: the entry of the list of biases that names an id, counted from 1 (0: none).
+template <int DT, class BiasOf>
+__device__ __forceinline__ void process_vec(const ProcArgs& a, const SeqParams& p, int b, int ctx, int t0, const Used<Logit<DT>::kPerVec>& u,
+                                            uint32_t special, uint32_t may, BiasOf bias_of, float (&x)[Logit<DT>::kPerVec]) {
     constexpr int N = Logit<DT>::kPerVec;
     if ((u.bits | special) != 0u) {
 #pragma unroll
@@ -204,8 +205,8 @@ __device__ __forceinline__ void process_vec(const ProcArgs& a, const SeqParams& 
                 }
             }
             if (used) x[e] = penalised(x[e], n, p);
-            if ((special >> e & 1u) && a.bias_offsets != nullptr) {
-                const int k = s.bias[t0 + e - lo];
+            if (special >> e & 1u) {
+                const int k = bias_of(t0 + e);
                 if (k > 0) x[e] = __fadd_rn(x[e], __ldg(a.bias_values + __ldg(a.bias_offsets + b) + k - 1));
             }
         }
@@ -249,7 +250,7 @@ __global__ void __launch_bounds__(kProcThreads) fsd_process_kernel(const ProcArg
         const uint32_t may = a.allowed != nullptr ? bits8(a.allowed + (static_cast<size_t>(b) * (a.P + 1) + ctx) * a.W, t0, 4 * a.W) : 0xffu;
         if (s != lies) { u = load_used<N>(a, b, t0); lies = s; }
         const uint32_t sp = special.any ? bits8(special.bits, t0 - lo, sizeof(special.bits)) & ((1u << N) - 1u) : 0u;
-        process_vec<DT, kSpan>(a, p, b, ctx, t0, lo, u, sp, may, special, x);
+        process_vec<DT>(a, p, b, ctx, t0, u, sp, may, [&](int t) { return a.bias_offsets != nullptr ? special.bias[t - lo] : 0; }, x);
         store_ids<DT>(out, t0, a.V, whole && alike, pack_vec<DT>(x));
     }
 }

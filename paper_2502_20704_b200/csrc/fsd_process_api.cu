@@ -3,6 +3,7 @@
 #include <climits>
 #include <cstdint>
 #include <cuda_runtime.h>
+#include <mutex>
 
 #include "fsd_verify.h"
 #include "fsd_device.cuh"
@@ -41,12 +42,57 @@ int check(const fsd_process_opts* o) {
     return FSD_OK;
 }
 
+// Rows that are cut off: a cluster of blocks holds a row in shared memory where it fits, else a block sweeps over it in memory.
+template <int DT>
+int launch_cut(const ProcArgs& a, bool raw, cudaStream_t s) {
+    constexpr int kDevices = 64;
+    constexpr size_t kMost = 200 * 1024;                  // of dynamic shared memory; the kernel has 7 KB of its own
+    static bool ready[kDevices] = {};
+    static std::mutex mu;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices) return FSD_ERR_CUDA;
+    {
+        std::lock_guard<std::mutex> lock(mu);
+        if (!ready[dev]) {
+            if (cudaFuncSetAttribute(fsd_cut_kernel<DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kMost)) != cudaSuccess) return FSD_ERR_CUDA;
+            ready[dev] = true;
+        }
+    }
+    const long long rows = static_cast<long long>(a.B) * (a.rows[0] + a.rows[1]);
+    // a row's vectors, wherever it starts
+    const int vecs = (a.V + 2 * (Logit<DT>::kPerVec - 1)) / Logit<DT>::kPerVec;
+    const size_t bins = kBins * sizeof(uint32_t);
+    int blocks = 1;
+    while (blocks < kMaxCutCluster && (vecs > blocks * 4096 || (rows * blocks < 2 * kSMs && vecs > blocks * 512))) blocks <<= 1;
+    const int slice = (vecs + blocks - 1) / blocks;
+    const size_t smem = static_cast<size_t>(slice) * 16 + bins;
+    if (smem > kMost) {
+        if (rows > INT_MAX) return FSD_ERR_SHAPE;
+        fsd_cut_long_kernel<DT><<<static_cast<unsigned>(rows), kLongThreads, 0, s>>>(a);
+        return cudaGetLastError() == cudaSuccess ? FSD_OK : FSD_ERR_CUDA;
+    }
+    if (rows * blocks > INT_MAX) return FSD_ERR_SHAPE;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(rows * blocks), 1, 1);
+    cfg.blockDim = dim3(kRowThreads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = static_cast<unsigned>(blocks); attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, fsd_cut_kernel<DT>, a, slice, raw) == cudaSuccess ? FSD_OK : FSD_ERR_CUDA;
+}
+
 template <int DT>
 int launch(const ProcArgs& a, bool cut, cudaStream_t s) {
-    const int per_block = kProcThreads * Logit<DT>::kPerVec;
     const int all = a.rows[0] + a.rows[1];
-    // a row's last vector may lie one further than its length says (see the kernel)
-    const long long spans = (a.V + Logit<DT>::kPerVec - 1 + per_block - 1) / per_block;
+    // a row's vectors, wherever it starts, by blocks
+    const long long spans = (a.V + 2 * (Logit<DT>::kPerVec - 1)) / Logit<DT>::kPerVec / kProcThreads + 1;
+    // The cut kernel does the rest too where the row stays on chip and there are no biases (whose lookup wants room there).
+    const bool together = cut && a.bias_offsets == nullptr && static_cast<long long>(a.V) * sizeof(typename Logit<DT>::elem) < kMaxCutCluster * 180000ll;
+    if (together) return launch_cut<DT>(a, false, s);
     // as many rows a block as leave eight blocks an SM, so that the counts are read for many rows at once
     long long group = spans * a.B * all / (8 * kSMs);
     group = group < 1 ? 1 : group > all ? all : group;
@@ -54,11 +100,7 @@ int launch(const ProcArgs& a, bool cut, cudaStream_t s) {
     if (spans * groups * a.B > INT_MAX) return FSD_ERR_SHAPE;
     fsd_process_kernel<DT><<<static_cast<unsigned>(spans * groups * a.B), kProcThreads, 0, s>>>(a, static_cast<int>(spans), static_cast<int>(groups), static_cast<int>(group));
     if (cudaGetLastError() != cudaSuccess) return FSD_ERR_CUDA;
-    if (cut) {
-        fsd_truncate_kernel<DT><<<static_cast<unsigned>(a.B) * all, kCutThreads, 0, s>>>(a);
-        if (cudaGetLastError() != cudaSuccess) return FSD_ERR_CUDA;
-    }
-    return FSD_OK;
+    return cut ? launch_cut<DT>(a, true, s) : FSD_OK;
 }
 
 int process(const void* target_in, const void* draft_in, const int32_t* parent, const int32_t* tokens, int B, int P, int V,

@@ -1,5 +1,11 @@
 // Top-k, top-p and min-p on rows of processed logits.
+//
+// The tokens that are kept are those above a value, the cut, and the first `ties` by id of those equal to it.  What decides
+// about a token near the border of top-p is a sum over the row to within that token's own weight, a millionth of the
+// whole in a flat row of 150000: sums are in double precision, and whether two programs agree never hangs on their order.
 #pragma once
+
+#include <type_traits>
 
 #include "fsd_process.cuh"
 
@@ -9,6 +15,7 @@ namespace fsd {
 // A key rises with the value, -0 and 0 have the same, and all of a type's values have keys of kKeyBits.
 template <int DT> constexpr int kKeyBits = DT == FSD_BF16 ? 16 : 32;
 template <int DT> constexpr uint32_t kSignBit = DT == FSD_BF16 ? 0x8000u : 0x80000000u;
+template <int DT> using LogitWord = typename std::conditional<DT == FSD_BF16, uint16_t, uint32_t>::type;
 template <int DT>
 __device__ __forceinline__ uint32_t key_of(uint32_t bits) {
     if (bits == kSignBit<DT>) bits = 0u;
@@ -20,13 +27,127 @@ __device__ __forceinline__ float value_of(uint32_t key) {
     return __uint_as_float(DT == FSD_BF16 ? bits << 16 : bits);
 }
 template <int DT> __device__ __forceinline__ uint32_t key_of_value(float y) { return key_of<DT>(__float_as_uint(y) >> (DT == FSD_BF16 ? 16 : 0)); }
-
-constexpr int kCutThreads = 1024;
+template <int DT> __device__ __forceinline__ float float_of(uint32_t word) { return __uint_as_float(DT == FSD_BF16 ? word << 16 : word); }
 
 struct CountAndWeight {
     long long n;
     double w;
 };
+
+// What a sequence asks for.
+struct CutParams {
+    int top_k;
+    float top_p, min_p;
+    bool k, p, m;
+};
+__device__ __forceinline__ CutParams cut_params(const ProcArgs& a, int b) {
+    CutParams c;
+    c.top_k = a.top_k != nullptr ? __ldg(a.top_k + b) : 0;
+    c.top_p = a.top_p != nullptr ? __ldg(a.top_p + b) : 1.f;
+    c.min_p = a.min_p != nullptr ? __ldg(a.min_p + b) : 0.f;
+    c.k = c.top_k > 0 && c.top_k < a.V;
+    c.p = c.top_p < 1.f;
+    c.m = c.min_p > 0.f;
+    return c;
+}
+
+// Of tokens of weight w behind others that weigh `above`: how many have predecessors that weigh less than the goal (at least one).
+__device__ __forceinline__ long long ties_below(double above, double w, double goal, int V) {
+    double j = ceil((goal - above) / w);
+    if (j >= 1.0 && above + (j - 1.0) * w >= goal) j -= 1.0;
+    if (above + j * w < goal) j += 1.0;
+    return j < 1.0 ? 1 : j > static_cast<double>(V) ? V : static_cast<long long>(j);
+}
+
+// The smallest key whose value is no further below the largest, `most` with key `top`, than ln(min_p).
+template <int DT>
+__device__ __forceinline__ uint32_t min_p_key(float min_p, uint32_t top, double most) {
+    const double far = log(static_cast<double>(min_p < 1.f ? min_p : 1.f));
+    uint32_t lo = key_of_value<DT>(-INFINITY), hi = top;        // hi always is, lo never
+    while (hi - lo > 1u) {
+        const uint32_t mid = lo + (hi - lo) / 2u;
+        if (static_cast<double>(value_of<DT>(mid)) - most >= far) hi = mid; else lo = mid;
+    }
+    return hi;
+}
+
+// ---- a bit at a time: rows of any length and any values -------------------------------
+// The cut is the largest key t for which the tokens at or above it are enough of what is asked for, found from its highest
+// bit down: a sweep over the row for each.  `row`: n words that this block has of the row, the first of them token first's;
+// total / largest: over all blocks that have some of the row.  Where only some of the tokens at the cut are kept, `until` is the id
+// from which on they are not.
+struct Cut {
+    bool any;
+    uint32_t key;
+    int until;
+};
+template <int DT, class Total, class Largest>
+__device__ Cut find_cut(const LogitWord<DT>* row, int n, int first, int V, const CutParams& c, Total total, Largest largest) {
+    const int tid = threadIdx.x, step = blockDim.x;
+    uint32_t top = 0u;
+    for (int i = tid; i < n; i += step) {
+        const uint32_t bits = row[i];
+        const float y = float_of<DT>(bits);
+        const uint32_t k = y != y ? 0xffffffffu : key_of<DT>(bits);
+        top = top > k ? top : k;
+    }
+    top = largest(top);
+    if (top >= key_of_value<DT>(INFINITY) || top <= key_of_value<DT>(-INFINITY)) return {false, 0u, 0};
+    const double most = value_of<DT>(top);
+    const auto weight = [&](uint32_t key) { return exp(static_cast<double>(value_of<DT>(key)) - most); };
+    // tokens with keys of at least t: how many, and (with weights) what those above `over` weigh
+    const auto at_least = [&](uint32_t t, uint32_t over, bool weights) {
+        CountAndWeight v = {0, 0.0};
+        for (int i = tid; i < n; i += step) {
+            const uint32_t k = key_of<DT>(row[i]);
+            if (k >= t) {
+                ++v.n;
+                if (weights && k > over) v.w += weight(k);
+            }
+        }
+        return total(v);
+    };
+
+    uint32_t cut = 0u;                 // tokens above it are kept, and of those equal to it the first `ties`
+    long long ties = V;
+    if (c.k) {
+        for (int bit = kKeyBits<DT> - 1; bit >= 0; --bit)
+            if (at_least(cut | 1u << bit, 0u, false).n >= c.top_k) cut |= 1u << bit;
+        ties = c.top_k - at_least(cut + 1u, 0u, false).n;
+    }
+    if (c.p) {
+        // what the top_k tokens weigh that are at or above t
+        const uint32_t over = c.k ? cut : 0u;
+        const double of_ties = c.k ? static_cast<double>(ties) * weight(cut) : 0.0;
+        const auto share = [&](uint32_t t) { return at_least(t, over, true).w + (c.k && t <= cut ? of_ties : 0.0); };
+        const double goal = static_cast<double>(c.top_p) * share(0u);
+        uint32_t t = 0u;
+        for (int bit = kKeyBits<DT> - 1; bit >= 0; --bit)
+            if (share(t | 1u << bit) >= goal) t |= 1u << bit;
+        if (!(goal > 0.0) || t > top) t = top;
+        const long long at_t = ties_below(t < top ? share(t + 1u) : 0.0, weight(t), goal, V);
+        ties = t > cut ? at_t : ties < at_t ? ties : at_t;
+        cut = t > cut ? t : cut;
+    }
+    if (c.m) {
+        const uint32_t t = min_p_key<DT>(c.min_p, top, most);
+        if (t > cut) { cut = t; ties = V; }
+    }
+    int until = V;
+    const long long equal = at_least(cut, 0u, false).n - at_least(cut + 1u, 0u, false).n;
+    if (ties < equal) {
+        int lo = 0, hi = V;                                 // the smallest id with `ties` of them in front of it
+        while (lo < hi) {
+            const int mid = lo + (hi - lo) / 2;
+            CountAndWeight v = {0, 0.0};
+            for (int i = tid; i < n && first + i < mid; i += step) v.n += key_of<DT>(row[i]) == cut;
+            if (total(v).n >= ties) hi = mid; else lo = mid + 1;
+        }
+        until = lo;
+    }
+    return {true, cut, until};
+}
+
 // Sums over the block in a fixed order; all threads have them.
 __device__ __forceinline__ CountAndWeight block_total(CountAndWeight v, CountAndWeight* scratch) {
 #pragma unroll
@@ -42,110 +163,667 @@ __device__ __forceinline__ CountAndWeight block_total(CountAndWeight v, CountAnd
     __syncthreads();
     return t;
 }
+__device__ __forceinline__ uint32_t block_largest(uint32_t k, CountAndWeight* scratch) {
+    k = __reduce_max_sync(0xffffffffu, k);
+    const int warps = blockDim.x >> 5;
+    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5].n = k;
+    __syncthreads();
+    for (int w = 0; w < warps; ++w) k = k > static_cast<uint32_t>(scratch[w].n) ? k : static_cast<uint32_t>(scratch[w].n);
+    __syncthreads();
+    return k;
+}
 
-// A block per row, in place.  Thresholds are found a bit at a time: the largest key t for which the tokens at or above it are
-// enough of what is asked for.  Every step is a sweep over the row, which is in the L2 cache after the first.
+// A block per row, in place, on rows that are too long for shared memory.
+constexpr int kLongThreads = 1024;
 template <int DT>
-__global__ void __launch_bounds__(kCutThreads) fsd_truncate_kernel(const ProcArgs a) {
-    using elem = typename Logit<DT>::elem;
-    using word = typename std::conditional<DT == FSD_BF16, uint16_t, uint32_t>::type;
+__global__ void __launch_bounds__(kLongThreads) fsd_cut_long_kernel(const ProcArgs a) {
     __shared__ CountAndWeight scratch[32];
     const int all = a.rows[0] + a.rows[1], b = blockIdx.x / all, q = blockIdx.x % all;
     const int side = q >= a.rows[0], r = q - (side ? a.rows[0] : 0);
-    const int V = a.V;
-    elem* out = static_cast<elem*>(a.out[side]) + (static_cast<size_t>(b) * a.rows[side] + r) * V;
-    const word* row = reinterpret_cast<const word*>(out);
-
-    const int top_k = a.top_k != nullptr ? __ldg(a.top_k + b) : 0;
-    const float top_p = a.top_p != nullptr ? __ldg(a.top_p + b) : 1.f, min_p = a.min_p != nullptr ? __ldg(a.min_p + b) : 0.f;
-    const bool cut_k = top_k > 0 && top_k < V, cut_p = top_p < 1.f, cut_m = min_p > 0.f;
-    if (!cut_k && !cut_p && !cut_m) return;
-
-    // the largest value; rows without a distribution are left as they are
-    const uint32_t kPosInf = key_of_value<DT>(INFINITY), kNegInf = key_of_value<DT>(-INFINITY);
-    uint32_t top = 0u;
-    for (int i = threadIdx.x; i < V; i += kCutThreads) {
-        const uint32_t bits = row[i];
-        const float y = __uint_as_float(DT == FSD_BF16 ? bits << 16 : bits);
-        const uint32_t k = y != y ? 0xffffffffu : key_of<DT>(bits);
-        top = top > k ? top : k;
+    LogitWord<DT>* row = static_cast<LogitWord<DT>*>(a.out[side]) + (static_cast<size_t>(b) * a.rows[side] + r) * a.V;
+    const CutParams c = cut_params(a, b);
+    if (!c.k && !c.p && !c.m) return;
+    const Cut cut = find_cut<DT>(row, a.V, 0, a.V, c, [&](CountAndWeight v) { return block_total(v, scratch); }, [&](uint32_t k) { return block_largest(k, scratch); });
+    if (!cut.any) return;
+    for (int i = threadIdx.x; i < a.V; i += kLongThreads) {
+        const uint32_t k = key_of<DT>(row[i]);
+        if (k < cut.key || (k == cut.key && i >= cut.until)) row[i] = static_cast<LogitWord<DT>>(__float_as_uint(-INFINITY) >> (DT == FSD_BF16 ? 16 : 0));
     }
-    top = __reduce_max_sync(0xffffffffu, top);
-    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5].n = top;
-    __syncthreads();
-    for (int w = 0; w < kCutThreads / 32; ++w) top = top > static_cast<uint32_t>(scratch[w].n) ? top : static_cast<uint32_t>(scratch[w].n);
-    __syncthreads();
-    if (top >= kPosInf || top <= kNegInf) return;
-    const double most = value_of<DT>(top);
-    const auto weight = [&](uint32_t key) { return exp(static_cast<double>(value_of<DT>(key)) - most); };
+}
 
-    // tokens with keys of at least t: how many, and (with weights) what those above `over` weigh
-    const auto at_least = [&](uint32_t t, uint32_t over, bool weights) {
-        CountAndWeight v = {0, 0.0};
-        for (int i = threadIdx.x; i < V; i += kCutThreads) {
-            const uint32_t k = key_of<DT>(row[i]);
-            if (k >= t) {
-                ++v.n;
-                if (weights && k > over) v.w += weight(k);
+// ---- rows that fit on chip: a cluster of blocks per row ---------------------------
+// A block reads its slice of the row once, processes it and keeps it in shared memory.  On the way it counts the values by their
+// upper 16 bits: for bf16 a bin is one value, so that the counts alone say where every cut is and what everything weighs, with
+// one exponential for a bin instead of one for a token.  For fp32 the bin of the border is split twice more by 8 bits.  The
+// first block of the cluster gets all counts (additions into its shared memory, whole numbers, so that their order does
+// not matter), finds the cut and tells the others.
+// Bins of one value are those of magnitudes from 2^-8 up to 2^7; smaller ones share a bin a sign and are weighed one by one, and where
+// a border lies in one of these, or something lies above, the row is cut a bit at a time.
+constexpr int kRowThreads = 512;
+constexpr int kRowWarps = kRowThreads / 32;
+constexpr int kMaxCutCluster = 8;
+constexpr uint32_t kMagLo = 0x3b7f, kMagHi = 0x4300;       // upper halves: just below 2^-8, and 2^7
+constexpr int kHalfBins = static_cast<int>(kMagHi - kMagLo) + 1;
+constexpr int kBins = 2 * kHalfBins;                       // negative magnitudes falling, then positive ones rising
+constexpr int kBinUnder = 0, kBinOver = kBins - 1, kBinTinyNeg = kHalfBins - 1, kBinTinyPos = kHalfBins;
+constexpr int kBinsEach = (kBins + kRowThreads - 1) / kRowThreads;
+constexpr double kFixed = 4398046511104.0;                 // 2^42: weights of a bin's tokens as whole numbers
+
+// The upper 16 bits of the keys of a one-value bin, and back.
+__device__ __forceinline__ uint32_t bin_prefix(int bin) {
+    return bin >= kHalfBins ? 0x8000u | (kMagLo + static_cast<uint32_t>(bin - kHalfBins)) : 0x7fffu ^ (kMagLo + static_cast<uint32_t>(kHalfBins - 1 - bin));
+}
+__device__ __forceinline__ bool one_value(int bin) { return bin != kBinUnder && bin != kBinOver && bin != kBinTinyNeg && bin != kBinTinyPos; }
+// The value of a bin: bf16 its only one, fp32 the middle of its range.
+template <int DT>
+__device__ __forceinline__ double bin_value(int bin) {
+    if constexpr (DT == FSD_BF16) return value_of<FSD_BF16>(bin_prefix(bin));
+    else return value_of<FSD_F32>(bin_prefix(bin) << 16 | 0x8000u);
+}
+
+enum CutKind { kCutNone, kCutDone, kCutByBits, kCutRefineK, kCutRefineP };
+struct CutResult {
+    int kind;
+    uint32_t key;              // of the cut; while it is being refined, its upper bits
+    long long ties;
+    uint32_t over;             // refining top-p: the tokens above this key are in the top_k
+};
+struct CutShared {
+    double tiny[kMaxCutCluster], above[kMaxCutCluster], rest[kMaxCutCluster];
+    uint32_t top[kMaxCutCluster];
+    int equal[kMaxCutCluster];
+    CountAndWeight slots[2][kMaxCutCluster];
+    CountAndWeight scratch[32];
+    uint64_t sub_w[256];
+    uint32_t sub_n[256];
+    CutResult work;            // the first block's
+    CutResult told[2];         // what the first block told last, and the time before
+    int found[4];
+    double goal, above_goal;
+    int warp_equal[kRowWarps + 1];
+    uint32_t special[256];     // a bit per 2^k vectors of the slice that hold a drafted token
+    int any_special;
+};
+
+template <int DT> struct RowSlice {
+    uint4* vecs;
+    int n;                     // vectors
+    int first;                 // id of the first one's first token
+};
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+__device__ __forceinline__ void cluster_barrier() { cluster_arrive(); cluster_wait(); }
+
+// Exclusive sums over the threads of the block, in thread order.  All threads; ends with a barrier.
+__device__ __forceinline__ CountAndWeight scan_threads(CountAndWeight v, CountAndWeight* scratch, CountAndWeight& all) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    CountAndWeight s = v;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const long long n = __shfl_up_sync(0xffffffffu, s.n, d);
+        const double w = __shfl_up_sync(0xffffffffu, s.w, d);
+        if (lane >= d) { s.n += n; s.w += w; }
+    }
+    if (lane == 31) scratch[warp] = s;
+    CountAndWeight e;
+    e.n = __shfl_up_sync(0xffffffffu, s.n, 1);
+    e.w = __shfl_up_sync(0xffffffffu, s.w, 1);
+    if (lane == 0) e = {0, 0.0};
+    __syncthreads();
+    all = {0, 0.0};
+    const int warps = blockDim.x >> 5;
+    for (int w = 0; w < warps; ++w) {
+        if (w == warp) { e.n += all.n; e.w += all.w; }
+        all.n += scratch[w].n; all.w += scratch[w].w;
+    }
+    __syncthreads();
+    return e;
+}
+
+// The first block: from the counts of all to the cut (bf16) or to the bins that hold the cuts (fp32).
+template <int DT>
+__device__ void solve_bins(const uint32_t* hist, CutShared& s, const CutParams& c, int blocks, int V) {
+    const int tid = threadIdx.x;
+    if (tid < 4) s.found[tid] = tid == 0 ? -1 : kBins;       // 0: bin of the k-th, 1: place of the highest bin, 2: place of the border of top-p
+    uint32_t n[kBinsEach];
+    CountAndWeight mine = {0, 0.0};
+    double w[kBinsEach];
+    double tiny = 0.0;
+    for (int k = 0; k < blocks; ++k) tiny += s.tiny[k];
+#pragma unroll
+    for (int j = 0; j < kBinsEach; ++j) {
+        const int bin = kBins - 1 - (tid * kBinsEach + j);
+        n[j] = bin >= 0 ? hist[bin] : 0u;
+        w[j] = 0.0;
+        if (n[j] != 0u && one_value(bin)) w[j] = exp(bin_value<DT>(bin));
+        mine.n += n[j];
+        mine.w += bin == kBinTinyPos ? tiny : n[j] * w[j];
+    }
+    if (tid == 0) s.work = {kCutDone, 0u, V, 0u};
+    CountAndWeight all;
+    const CountAndWeight before = scan_threads(mine, s.scratch, all);
+    const bool cut_k = c.k && all.n > c.top_k;
+    // the highest bin, and that of the k-th token
+    CountAndWeight run = before;
+#pragma unroll
+    for (int j = 0; j < kBinsEach; ++j) {
+        const int place = tid * kBinsEach + j, bin = kBins - 1 - place;
+        if (n[j] != 0u) {
+            if (run.n == 0) s.found[1] = place;
+            if (cut_k && run.n < c.top_k && run.n + n[j] >= c.top_k) {
+                s.found[0] = place;
+                s.work.ties = c.top_k - run.n;
+                s.above_goal = run.w;                       // what stands above this bin weighs
+                if (one_value(bin)) s.goal = run.w + static_cast<double>(c.top_k - run.n) * w[j];
             }
         }
-        return block_total(v, scratch);
-    };
+        run.n += n[j];
+        run.w += bin == kBinTinyPos ? tiny : n[j] * w[j];
+    }
+    __syncthreads();
+    const int top_bin = kBins - 1 - s.found[1], k_place = s.found[0], k_bin = kBins - 1 - k_place;
+    if (all.n == 0) {                                       // nothing finite, and nothing above it either
+        if (tid == 0) s.work.kind = kCutNone;
+        __syncthreads();
+        return;
+    }
+    double most;
+    uint32_t top;
+    if constexpr (DT == FSD_BF16) {
+        top = bin_prefix(top_bin);
+        most = one_value(top_bin) ? bin_value<DT>(top_bin) : 0.0;
+    } else {
+        top = 0u;
+        for (int k = 0; k < blocks; ++k) top = top > s.top[k] ? top : s.top[k];
+        most = value_of<FSD_F32>(top);
+    }
+    // Values off the bins: above them, or a border in a bin of many; below them what is worth nothing beside a highest value of
+    // at least -60 (e^-68 of it each) and is nothing but a count.
+    if (hist[kBinOver] != 0u || !one_value(top_bin) || (hist[kBinUnder] != 0u && most < -60.0) || (cut_k && !one_value(k_bin))) {
+        if (tid == 0) s.work.kind = kCutByBits;
+        __syncthreads();
+        return;
+    }
+    // top-p: the first place at which the tokens so far weigh the goal
+    const double share = cut_k ? s.goal : all.w, goal = static_cast<double>(c.top_p) * share;
+    if (c.p) {
+        run = before;
+#pragma unroll
+        for (int j = 0; j < kBinsEach; ++j) {
+            const int place = tid * kBinsEach + j, bin = kBins - 1 - place;
+            run.w += bin == kBinTinyPos ? tiny : n[j] * w[j];
+            if (n[j] != 0u && run.w >= goal) { atomicMin(&s.found[2], place); break; }
+        }
+        __syncthreads();
+    }
+    int p_place = s.found[2];
+    if (cut_k && p_place > k_place) p_place = k_place;
+    if (c.p && !(goal > 0.0)) p_place = s.found[1];
+    if (p_place >= kBins) p_place = kBins - 1;              // (not reached: the goal is below the whole)
+    const int p_bin = kBins - 1 - p_place;
+    if (c.p && !one_value(p_bin)) {
+        if (tid == 0) s.work.kind = kCutByBits;
+        __syncthreads();
+        return;
+    }
+    if constexpr (DT == FSD_BF16) {
+        // the thread that has the border's bin
+        if (c.p && p_place / kBinsEach == tid) {
+            run = before;
+#pragma unroll
+            for (int j = 0; j < kBinsEach; ++j) {
+                const int bin = kBins - 1 - (tid * kBinsEach + j);
+                if (bin == p_bin) {
+                    const long long t = ties_below(run.w, w[j], goal, V);
+                    const long long k_ties = s.work.ties;
+                    s.work.ties = cut_k && p_place == k_place && k_ties < t ? k_ties : t;
+                    s.work.key = bin_prefix(bin);
+                    if (s.work.ties >= n[j]) s.work.ties = V;       // all of them
+                }
+                run.w += bin == kBinTinyPos ? tiny : n[j] * w[j];
+            }
+        } else if (!c.p && cut_k && k_place / kBinsEach == tid) {
+            s.work.key = bin_prefix(k_bin);
+            if (s.work.ties >= hist[k_bin]) s.work.ties = V;
+        }
+        __syncthreads();
+        if (tid == 0 && c.m) {
+            const uint32_t t = min_p_key<DT>(c.min_p, top, most);
+            if (t > s.work.key) { s.work.key = t; s.work.ties = V; }
+        }
+        if (tid == 0 && s.work.key == 0u) s.work.kind = kCutNone;
+    } else {
+        if (tid == 0) {
+            s.found[3] = p_bin;
+            if (cut_k) {
+                s.work.kind = kCutRefineK;
+                s.work.key = bin_prefix(k_bin);
+            } else if (c.p) {
+                s.work.kind = kCutRefineP;
+                s.work.key = bin_prefix(p_bin);
+            } else if (c.m) {
+                s.work.key = min_p_key<DT>(c.min_p, top, most);
+            } else {
+                s.work.kind = kCutNone;                     // (fewer tokens than top_k)
+            }
+        }
+    }
+    __syncthreads();
+}
 
-    uint32_t cut = 0u;                 // tokens above it are kept, and of those equal to it the first `ties`
-    long long ties = V;
+// Counts, by the 8 bits above `shift`, the tokens whose keys have the upper bits `prefix` and are above `over`; with weights also
+// what they weigh against the largest value of the bin's range (whole numbers of 1 / kFixed), and what all tokens above and below the
+// prefix weigh against `most`.  All into the first block's shared memory.
+template <bool WEIGHTS>
+__device__ void count_bits(const RowSlice<FSD_F32>& row, CutShared& s, CutShared& first, int rank, uint32_t prefix, int shift, uint32_t over, double most) {
+    const int tid = threadIdx.x;
+    if (rank != 0) {
+        for (int i = tid; i < 256; i += kRowThreads) { s.sub_n[i] = 0u; s.sub_w[i] = 0u; }
+        __syncthreads();
+    }
+    const double edge = value_of<FSD_F32>(prefix << (shift + 8) | ((1u << (shift + 8)) - 1u));
+    CountAndWeight above = {0, 0.0}, rest = {0, 0.0};
+    for (int i = tid; i < row.n; i += kRowThreads) {
+        const uint4 v = row.vecs[i];
+        const uint32_t bits[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t k = key_of<FSD_F32>(bits[e]), high = k >> (shift + 8);
+            if (WEIGHTS && bits[e] != 0xff800000u && k > over) {
+                if (high != prefix) {
+                    const double w = exp(static_cast<double>(__uint_as_float(bits[e])) - most);
+                    if (high > prefix) above.w += w; else rest.w += w;
+                }
+            }
+            if (high == prefix && k > over) {
+                const uint32_t bin = k >> shift & 255u;
+                atomicAdd(&s.sub_n[bin], 1u);
+                if (WEIGHTS)
+                    atomicAdd(reinterpret_cast<unsigned long long*>(&s.sub_w[bin]),
+                              static_cast<unsigned long long>(__double2ull_rn(exp(static_cast<double>(__uint_as_float(bits[e])) - edge) * kFixed)));
+            }
+        }
+    }
+    if (WEIGHTS) {
+        above = block_total(above, s.scratch);
+        rest = block_total(rest, s.scratch);
+        if (tid == 0) { first.above[rank] = above.w; first.rest[rank] = rest.w; }
+    }
+    __syncthreads();
+    if (rank != 0)
+        for (int i = tid; i < 256; i += kRowThreads)
+            if (s.sub_n[i] != 0u) {
+                atomicAdd(&first.sub_n[i], s.sub_n[i]);
+                if (WEIGHTS) atomicAdd(reinterpret_cast<unsigned long long*>(&first.sub_w[i]), static_cast<unsigned long long>(s.sub_w[i]));
+            }
+}
+
+// The first block tells the others what it found, and clears the counts for the next time.  Two places in turn: a block may still
+// be reading what it was told before.
+__device__ __forceinline__ CutResult tell_result(CutShared& s, cg::cluster_group& cluster, int rank, int blocks, int& turn) {
+    turn ^= 1;
+    if (rank == 0) {
+        const int tid = threadIdx.x;
+        __syncthreads();
+        if (tid < blocks) *cluster.map_shared_rank(&s.told[turn], tid) = s.work;
+        for (int i = tid; i < 256; i += kRowThreads) { s.sub_n[i] = 0u; s.sub_w[i] = 0u; }
+    }
+    cluster_barrier();
+    return s.told[turn];
+}
+
+// The next bin in use above (up) or below a bin; -1 if there is none.  All of the first block's threads.
+__device__ __forceinline__ int next_bin(const uint32_t* hist, CutShared& s, int bin, bool up) {
+    if (threadIdx.x == 0) s.found[0] = up ? kBins : -1;
+    __syncthreads();
+    for (int i = threadIdx.x; i < kBins; i += kRowThreads)
+        if (hist[i] != 0u) {
+            if (up && i > bin) atomicMin(&s.found[0], i);
+            if (!up && i < bin) atomicMax(&s.found[0], i);
+        }
+    __syncthreads();
+    const int found = s.found[0];
+    __syncthreads();
+    return found == kBins ? -1 : found;
+}
+
+__device__ __forceinline__ void at_least_min_p(CutShared& s, const CutParams& c, int V, uint32_t top) {       // one thread
+    const uint32_t t = min_p_key<FSD_F32>(c.min_p, top, value_of<FSD_F32>(top));
+    if (t > s.work.key) { s.work.key = t; s.work.ties = V; }
+}
+
+// fp32: from the bins of the cuts to the cuts.
+__device__ CutResult refine(const RowSlice<FSD_F32>& row, const uint32_t* hist, CutShared& s, CutShared& first, cg::cluster_group& cluster, int rank, int blocks,
+                            const CutParams& c, int V, uint32_t top, CutResult res, int& turn) {
+    const int tid = threadIdx.x;
+    const double most = value_of<FSD_F32>(top);
+    const bool cut_k = res.kind == kCutRefineK;
+    int p_bin = rank == 0 ? s.found[3] : 0;                 // (the first block's) the bin that may have the border of top-p
     if (cut_k) {
-        for (int bit = kKeyBits<DT> - 1; bit >= 0; --bit)
-            if (at_least(cut | 1u << bit, 0u, false).n >= top_k) cut |= 1u << bit;
-        ties = top_k - at_least(cut + 1u, 0u, false).n;
-    }
-    if (cut_p) {
-        // what the top_k tokens weigh that are at or above t
-        const uint32_t over = cut_k ? cut : 0u;
-        const double of_ties = cut_k ? static_cast<double>(ties) * weight(cut) : 0.0;
-        const auto share = [&](uint32_t t) { return at_least(t, over, true).w + (cut_k && t <= cut ? of_ties : 0.0); };
-        const double goal = static_cast<double>(top_p) * share(0u);
-        uint32_t t = 0u;
-        for (int bit = kKeyBits<DT> - 1; bit >= 0; --bit)
-            if (share(t | 1u << bit) >= goal) t |= 1u << bit;
-        if (!(goal > 0.0) || t > top) t = top;
-        // of the tokens at t: those whose predecessors weigh less than the goal
-        const double w = weight(t), above = t < top ? share(t + 1u) : 0.0;
-        double j = ceil((goal - above) / w);
-        if (j >= 1.0 && above + (j - 1.0) * w >= goal) j -= 1.0;
-        if (above + j * w < goal) j += 1.0;
-        const long long most_ties = j < 1.0 ? 1 : j > static_cast<double>(V) ? V : static_cast<long long>(j);
-        ties = t > cut ? most_ties : ties < most_ties ? ties : most_ties;
-        cut = t > cut ? t : cut;
-    }
-    if (cut_m) {
-        // the smallest key whose value is no further below the largest than ln(min_p)
-        const double far = log(static_cast<double>(min_p < 1.f ? min_p : 1.f));
-        uint32_t lo = kNegInf, hi = top;                    // hi always is, lo never
-        while (hi - lo > 1u) {
-            const uint32_t mid = lo + (hi - lo) / 2u;
-            if (static_cast<double>(value_of<DT>(mid)) - most >= far) hi = mid; else lo = mid;
+        for (int shift = 8; shift >= 0; shift -= 8) {
+            count_bits<false>(row, s, first, rank, res.key, shift, 0u, most);
+            cluster_barrier();
+            if (rank == 0) {
+                CountAndWeight all;
+                const int bin = 255 - tid;
+                const long long n = tid < 256 ? s.sub_n[bin] : 0;
+                const CountAndWeight before = scan_threads({n, 0.0}, s.scratch, all);
+                if (before.n < res.ties && before.n + n >= res.ties) {
+                    s.work.key = res.key << 8 | static_cast<uint32_t>(bin);
+                    s.work.ties = res.ties - before.n;
+                    if (shift == 0) s.work.over = s.work.ties >= n;            // whether all that are equal are kept
+                }
+                __syncthreads();
+                if (tid == 0 && shift == 0 && !c.p) {
+                    s.work.kind = kCutDone;
+                    if (s.work.over) s.work.ties = V;
+                    if (c.m) at_least_min_p(s, c, V, top);
+                }
+            }
+            res = tell_result(s, cluster, rank, blocks, turn);
         }
-        if (hi > cut) { cut = hi; ties = V; }
+        if (!c.p) return res;
+    }
+    // Tokens above `over` are in the top_k, and of those equal to it k_ties.
+    const uint32_t over = cut_k ? res.key : 0u;
+    const long long k_ties = cut_k ? res.ties : 0;
+    const bool all_of_k = cut_k && res.over;
+    const double of_ties = cut_k ? static_cast<double>(k_ties) * exp(static_cast<double>(value_of<FSD_F32>(over)) - most) : 0.0;
+    if (cut_k) {
+        if (rank == 0 && tid == 0) s.work = {kCutRefineP, bin_prefix(p_bin), 0, 0u};
+        res = tell_result(s, cluster, rank, blocks, turn);
+    }
+    // The bin is a guess, made with the middles of the bins; the sums say whether to move to the next one in use.  (Where rounding would
+    // send it back and forth, the border is between the two.)
+    int last_move = 0;
+    while (res.kind == kCutRefineP) {
+        const uint32_t prefix = res.key;
+        count_bits<true>(row, s, first, rank, prefix, 8, over, most);
+        cluster_barrier();
+        if (rank == 0) {
+            double above = 0.0, rest = 0.0;
+            for (int k = 0; k < blocks; ++k) { above += s.above[k]; rest += s.rest[k]; }
+            const double unit = exp(static_cast<double>(value_of<FSD_F32>(prefix << 16 | 0xffffu)) - most) / kFixed;
+            CountAndWeight all;
+            const int bin = 255 - tid;
+            const double w = tid < 256 ? static_cast<double>(s.sub_w[bin]) * unit : 0.0;
+            const long long n = tid < 256 ? s.sub_n[bin] : 0;
+            const CountAndWeight before = scan_threads({n, w}, s.scratch, all);
+            const double goal = static_cast<double>(c.top_p) * (above + all.w + rest + of_ties);
+            if (tid == 0) { s.found[1] = -1; s.found[2] = 256; }
+            __syncthreads();
+            if (n != 0) {
+                atomicMax(&s.found[1], tid);                                      // the last sub-bin in use
+                if (above + before.w + w >= goal) atomicMin(&s.found[2], tid);
+            }
+            __syncthreads();
+            int place = s.found[2];
+            bool up = goal > 0.0 && above >= goal, down = !up && place == 256;
+            if (down && s.found[1] >= 0 && last_move > 0) { place = s.found[1]; down = false; }
+            if (up && s.found[1] >= 0 && last_move < 0) up = false;               // (place is its first sub-bin in use)
+            if (down && cut_k && prefix <= over >> 16) {                          // the border is among the tokens equal to the k-th
+                if (tid == 0) {
+                    const long long t = ties_below(above + all.w, of_ties / static_cast<double>(k_ties), goal, V);
+                    s.work = {kCutDone, over, t < k_ties ? t : all_of_k ? V : k_ties, 0u};
+                }
+            } else if (up || down) {
+                p_bin = next_bin(hist, s, p_bin, up);
+                last_move = up ? 1 : -1;
+                if (tid == 0) {
+                    if (p_bin < 0 || !one_value(p_bin)) s.work.kind = kCutByBits;
+                    else s.work.key = bin_prefix(p_bin);
+                }
+            } else if (tid == place) {
+                s.work.key = prefix << 8 | static_cast<uint32_t>(bin);
+                s.work.kind = kCutRefineK;                                        // (the last 8 bits)
+                s.goal = goal;
+                s.above_goal = above + before.w;
+            }
+        }
+        res = tell_result(s, cluster, rank, blocks, turn);
+    }
+    if (res.kind == kCutRefineK) {
+        const uint32_t prefix = res.key;
+        count_bits<false>(row, s, first, rank, prefix, 0, over, most);
+        cluster_barrier();
+        if (rank == 0) {
+            CountAndWeight all;
+            const int bin = 255 - tid;
+            const uint32_t key = prefix << 8 | static_cast<uint32_t>(bin);
+            const long long n = tid < 256 ? s.sub_n[bin] : 0;
+            const double w = n != 0 ? exp(static_cast<double>(value_of<FSD_F32>(key)) - most) : 0.0;
+            const CountAndWeight before = scan_threads({n, static_cast<double>(n) * w}, s.scratch, all);
+            if (tid == 0) s.found[2] = 256;
+            __syncthreads();
+            // (where rounding leaves the last of them short of the goal it is the border all the same)
+            if (n != 0 && (s.above_goal + before.w + static_cast<double>(n) * w >= s.goal || before.n + n == all.n)) atomicMin(&s.found[2], tid);
+            __syncthreads();
+            if (tid == s.found[2]) {
+                const long long t = ties_below(s.above_goal + before.w, w, s.goal, V);
+                s.work = {kCutDone, key, t >= n ? V : t, 0u};
+            }
+            __syncthreads();
+        }
+    }
+    if (res.kind != kCutByBits && (res.kind == kCutRefineK || c.m)) {
+        if (rank == 0 && tid == 0 && c.m) at_least_min_p(s, c, V, top);
+        res = tell_result(s, cluster, rank, blocks, turn);
+    }
+    return res;
+}
+
+template <int DT>
+__device__ __forceinline__ void words_of(const uint4& v, uint32_t (&bits)[Logit<DT>::kPerVec]) {      // widened
+    if constexpr (DT == FSD_BF16) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) bits[e] = (e & 1) ? w[e / 2] & 0xffff0000u : w[e / 2] << 16;
+    } else {
+        bits[0] = v.x; bits[1] = v.y; bits[2] = v.z; bits[3] = v.w;
+    }
+}
+
+// raw: the rows are processed already.
+template <int DT>
+__global__ void __launch_bounds__(kRowThreads) fsd_cut_kernel(const ProcArgs a, int slice, bool raw) {
+    constexpr int N = Logit<DT>::kPerVec;
+    using elem = typename Logit<DT>::elem;
+    extern __shared__ uint4 on_chip[];
+    __shared__ CutShared s;
+    uint32_t* hist = reinterpret_cast<uint32_t*>(on_chip + slice);
+    cg::cluster_group cluster = cg::this_cluster();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int blocks = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
+    const int all = a.rows[0] + a.rows[1], line = blockIdx.x / blocks, b = line / all, q = line % all;
+    const int side = q >= a.rows[0], r = q - (side ? a.rows[0] : 0);
+    const size_t at = (static_cast<size_t>(b) * a.rows[side] + r) * a.V;
+    const elem* in = static_cast<const elem*>(raw ? a.out[side] : a.in[side]) + at;
+    elem* out = static_cast<elem*>(a.out[side]) + at;
+    const int lies = static_cast<int>(reinterpret_cast<uintptr_t>(in) % 16 / sizeof(elem));
+    const bool alike = (reinterpret_cast<uintptr_t>(in) ^ reinterpret_cast<uintptr_t>(out)) % 16 == 0;
+    const int row_vecs = (a.V + lies + N - 1) / N, v0 = rank * slice;
+    RowSlice<DT> row = {on_chip, row_vecs - v0 < slice ? (row_vecs > v0 ? row_vecs - v0 : 0) : slice, v0 * N - lies};
+
+    const CutParams c = cut_params(a, b);
+    const bool cutting = c.k || c.p || c.m;
+    const SeqParams p = seq_params(a, b);
+    const int ctx = context_row(a, b, side, r);
+    const int drafts = !raw && a.penalties && a.tokens != nullptr ? a.P : 0;
+    int coarse = 0;                                         // 2^coarse vectors a bit
+    while ((slice >> coarse) > 256 * 32) ++coarse;
+    for (int i = tid; i < kBins; i += kRowThreads) hist[i] = 0u;
+    if (tid < 256) { s.special[tid] = 0u; s.sub_n[tid] = 0u; s.sub_w[tid] = 0u; }
+    if (tid == 0) s.any_special = 0;
+    __syncthreads();
+    cluster_arrive();                                       // from here on others may add to the first block's counts
+    for (int j = tid; j < drafts; j += kRowThreads) {
+        const int t = __ldg(a.tokens + static_cast<size_t>(b) * a.P + j);
+        if (t >= 0 && t < a.V) {
+            const int v = (t + lies) / N - v0;
+            if (v >= 0 && v < row.n) {
+                atomicOr(&s.special[v >> coarse >> 5], 1u << (v >> coarse & 31));
+                s.any_special = 1;
+            }
+        }
+    }
+    __syncthreads();
+    const bool any_special = s.any_special != 0;
+
+    // the slice: read, processed, counted, kept
+    double tiny = 0.0;
+    uint32_t top = 0u;
+#pragma unroll 2
+    for (int i = tid; i < row.n; i += kRowThreads) {
+        const int t0 = row.first + i * N;
+        const bool whole = t0 >= 0 && t0 + N <= a.V;
+        float x[N];
+        load_ids<DT>(in, t0, a.V, whole, x);
+        if (!raw) {
+            const uint32_t may = a.allowed != nullptr ? bits8(a.allowed + (static_cast<size_t>(b) * (a.P + 1) + ctx) * a.W, t0, 4 * a.W) : 0xffu;
+            const Used<N> u = load_used<N>(a, b, t0);
+            const uint32_t sp = any_special && (s.special[i >> coarse >> 5] >> (i >> coarse & 31) & 1u) ? (1u << N) - 1u : 0u;
+            process_vec<DT>(a, p, b, ctx, t0, u, sp, may, [](int) { return 0; }, x);
+        }
+        const uint4 v = pack_vec<DT>(x);
+        if (!cutting) {
+            store_ids<DT>(out, t0, a.V, whole && alike, v);
+            continue;
+        }
+        uint32_t bits[N];
+        words_of<DT>(v, bits);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            if (!whole && (t0 + e < 0 || t0 + e >= a.V)) { bits[e] = 0xff800000u; continue; }
+            if (bits[e] == 0xff800000u) continue;
+            const uint32_t mag = bits[e] >> 16 & 0x7fffu;
+            uint32_t u = (mag < kMagLo ? kMagLo : mag > kMagHi ? kMagHi : mag) - kMagLo;
+            int bin = static_cast<int>(u ^ static_cast<uint32_t>(static_cast<int>(bits[e]) >> 31)) + kHalfBins;
+            if (u == 0u) tiny += exp(static_cast<double>(__uint_as_float(bits[e])));
+            if ((bits[e] & 0x7fffffffu) > 0x7f800000u) bin = kBinOver;
+            atomicAdd(&hist[bin], 1u);
+            if constexpr (DT == FSD_F32) { const uint32_t k = key_of<DT>(bits[e]); top = top > k ? top : k; }
+        }
+        if (whole) row.vecs[i] = v;
+        else if constexpr (DT == FSD_BF16)
+            row.vecs[i] = make_uint4(bits[0] >> 16 | bits[1], bits[2] >> 16 | bits[3], bits[4] >> 16 | bits[5], bits[6] >> 16 | bits[7]);
+        else row.vecs[i] = make_uint4(bits[0], bits[1], bits[2], bits[3]);
+    }
+    if (!cutting) { cluster_wait(); return; }               // (the whole cluster: it is the sequence that asks)
+
+    CutShared& first = *cluster.map_shared_rank(&s, 0);
+    const CountAndWeight tiny_all = block_total({0, tiny}, s.scratch);
+    if constexpr (DT == FSD_F32) top = block_largest(top, s.scratch);
+    cluster_wait();
+    if (tid == 0) { first.tiny[rank] = tiny_all.w; first.top[rank] = top; }
+    if (rank != 0) {
+        uint32_t* sums = cluster.map_shared_rank(hist, 0);
+        for (int i = tid; i < kBins; i += kRowThreads)
+            if (hist[i] != 0u) atomicAdd(sums + i, hist[i]);
+    }
+    cluster_barrier();
+    if (rank == 0) {
+        solve_bins<DT>(hist, s, c, blocks, a.V);
+        if (DT == FSD_F32 && tid > 0 && tid < blocks)
+            for (int k = 0; k < blocks; ++k) cluster.map_shared_rank(&s, tid)->top[k] = s.top[k];
+    }
+    int turn = 0;
+    CutResult res = tell_result(s, cluster, rank, blocks, turn);
+    if constexpr (DT == FSD_F32) {
+        if (res.kind == kCutRefineK || res.kind == kCutRefineP) {
+            top = 0u;
+            for (int k = 0; k < blocks; ++k) top = top > s.top[k] ? top : s.top[k];
+            res = refine(row, hist, s, first, cluster, rank, blocks, c, a.V, top, res, turn);
+        }
     }
 
-    // Where only some of the tokens at the cut are kept: the id from which on they are not.
-    int until = V;
-    const long long equal = at_least(cut, 0u, false).n - at_least(cut + 1u, 0u, false).n;
-    if (ties < equal) {
-        int lo = 0, hi = V;                                 // the smallest id with `ties` of them in front of it
-        while (lo < hi) {
-            const int mid = lo + (hi - lo) / 2;
-            CountAndWeight v = {0, 0.0};
-            for (int i = threadIdx.x; i < mid; i += kCutThreads) v.n += key_of<DT>(row[i]) == cut;
-            if (block_total(v, scratch).n >= ties) hi = mid; else lo = mid + 1;
-        }
-        until = lo;
+    uint32_t key = res.key;
+    int until = a.V;                                        // of the tokens at the cut, those from this id on are not kept
+    bool keep_all = res.kind == kCutNone;
+    if (res.kind == kCutByBits) {
+        const auto total = [&](CountAndWeight v) {
+            v = block_total(v, s.scratch);
+            turn ^= 1;
+            if (tid < blocks) cluster.map_shared_rank(&s, tid)->slots[turn][rank] = v;
+            cluster_barrier();
+            CountAndWeight t = {0, 0.0};
+            for (int k = 0; k < blocks; ++k) { t.n += s.slots[turn][k].n; t.w += s.slots[turn][k].w; }
+            return t;
+        };
+        const auto largest = [&](uint32_t k) {
+            k = block_largest(k, s.scratch);
+            turn ^= 1;
+            if (tid < blocks) cluster.map_shared_rank(&s, tid)->slots[turn][rank].n = k;
+            cluster_barrier();
+            for (int j = 0; j < blocks; ++j) k = k > static_cast<uint32_t>(s.slots[turn][j].n) ? k : static_cast<uint32_t>(s.slots[turn][j].n);
+            return k;
+        };
+        const Cut cut = find_cut<DT>(reinterpret_cast<const LogitWord<DT>*>(row.vecs), row.n * N, row.first, a.V, c, total, largest);
+        key = cut.key;
+        until = cut.until;
+        keep_all = !cut.any;
     }
-    const float none = -INFINITY;
-    for (int i = threadIdx.x; i < V; i += kCutThreads) {
-        const uint32_t k = key_of<DT>(row[i]);
-        if (k < cut || (k == cut && i >= until)) reinterpret_cast<word*>(out)[i] = static_cast<word>(__float_as_uint(none) >> (DT == FSD_BF16 ? 16 : 0));
+    const long long ties = res.kind == kCutDone ? res.ties : a.V;
+    const float value = value_of<DT>(key);
+    // where only the first `ties` of the tokens at the cut are kept, each warp has a run of the slice and counts those before it
+    const int run = (row.n + kRowWarps - 1) / kRowWarps, w0 = warp * run < row.n ? warp * run : row.n, w1 = w0 + run < row.n ? w0 + run : row.n;
+    long long before = 0;
+    if (ties < a.V) {
+        int mine = 0;
+        for (int i = w0 + lane; i < w1; i += 32) {
+            uint32_t bits[N];
+            words_of<DT>(row.vecs[i], bits);
+#pragma unroll
+            for (int e = 0; e < N; ++e) mine += __uint_as_float(bits[e]) == value;
+        }
+        mine = __reduce_add_sync(0xffffffffu, mine);
+        if (lane == 0) s.warp_equal[warp] = mine;
+        __syncthreads();
+        int sum = 0, ahead = 0;
+        for (int w = 0; w < kRowWarps; ++w) { if (w == warp) ahead = sum; sum += s.warp_equal[w]; }
+        if (tid < blocks) cluster.map_shared_rank(&s, tid)->equal[rank] = sum;
+        cluster_barrier();
+        for (int k = 0; k < rank; ++k) before += s.equal[k];
+        before += ahead;
+    }
+    for (int i0 = w0; i0 < w1; i0 += 32) {
+        const int i = i0 + lane;
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        uint32_t bits[N];
+        int equal = 0;
+        if (i < w1) v = row.vecs[i];
+        words_of<DT>(v, bits);
+        long long ahead = before;
+        if (ties < a.V) {
+            if (i < w1) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) equal += __uint_as_float(bits[e]) == value;
+            }
+            int sum = equal;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int o = __shfl_up_sync(0xffffffffu, sum, d);
+                if (lane >= d) sum += o;
+            }
+            ahead = before + sum - equal;
+            before += __shfl_sync(0xffffffffu, sum, 31);
+        }
+        if (i >= w1) continue;
+        const int t0 = row.first + i * N;
+        if (!keep_all) {
+            uint32_t out_bits[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float y = __uint_as_float(bits[e]);
+                bool keep = y > value || (y == value && t0 + e < until);
+                if (ties < a.V && y == value) { keep = ahead < ties; ++ahead; }
+                out_bits[e] = keep ? bits[e] : 0xff800000u;
+            }
+            if constexpr (DT == FSD_BF16)
+                v = make_uint4(out_bits[0] >> 16 | out_bits[1], out_bits[2] >> 16 | out_bits[3], out_bits[4] >> 16 | out_bits[5], out_bits[6] >> 16 | out_bits[7]);
+            else v = make_uint4(out_bits[0], out_bits[1], out_bits[2], out_bits[3]);
+        }
+        store_ids<DT>(out, t0, a.V, t0 >= 0 && t0 + N <= a.V && alike, v);
     }
 }
 

@@ -148,7 +148,7 @@ def test_cut_rows(B, P, V, steps, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("V", [32000, 50257, 128256, 256000])
+@pytest.mark.parametrize("V", [32000, 50257, 128256, 256000, 800001])
 def test_cut_long_rows(V, dtype):
     c = lg.Call(6, 0, V, dtype, ("temp", "k", "p", "m"), seed=21)
     c.o["top_k"] = np.array([0, 0, 50, V // 3, 0, 1000], np.int32)
