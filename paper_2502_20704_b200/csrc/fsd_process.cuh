@@ -3,6 +3,8 @@
 // form of the same operations has the same bits.
 #pragma once
 
+#include <climits>
+
 #include "fsd_device.cuh"
 
 namespace fsd {
@@ -115,23 +117,30 @@ __device__ void find_special(const ProcArgs& a, int b, int lo, Special<SPAN>& s)
     __syncthreads();
 }
 
-// The vector of logits that covers ids t0 .. t0 + N - 1 of a row, widened; ids outside [0, V) are left alone.
+// The vector of logits that covers ids t0 .. t0 + N - 1 of a row; ids outside [0, V) are -inf.
 template <int DT>
-__device__ __forceinline__ void load_ids(const void* row, int t0, int V, bool whole, float (&x)[Logit<DT>::kPerVec]) {
+__device__ __forceinline__ uint4 load_ids(const void* row, int t0, int V, bool whole) {
     constexpr int N = Logit<DT>::kPerVec;
-    if (whole) {
-        const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const typename Logit<DT>::elem*>(row) + t0);
-        unpack_vec<DT>(v, x);
-    } else {
+    if (whole) return *reinterpret_cast<const uint4*>(static_cast<const typename Logit<DT>::elem*>(row) + t0);
+    uint32_t w[4];
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            x[e] = 0.f;
-            if (t0 + e >= 0 && t0 + e < V) {
-                if constexpr (DT == FSD_BF16) x[e] = __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(row)[t0 + e]) << 16);
-                else x[e] = static_cast<const float*>(row)[t0 + e];
-            }
+    for (int k = 0; k < 4; ++k) w[k] = DT == FSD_BF16 ? 0xff80ff80u : 0xff800000u;
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+        if (t0 + e >= 0 && t0 + e < V) {
+            if constexpr (DT == FSD_BF16) w[e / 2] = __byte_perm(w[e / 2], static_cast<const uint16_t*>(row)[t0 + e], (e & 1) ? 0x5410u : 0x3254u);
+            else w[e] = static_cast<const uint32_t*>(row)[t0 + e];
         }
-    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Which of a vector's ids there are.
+template <int N>
+__device__ __forceinline__ uint32_t ids_of(int t0, int V) {
+    uint32_t m = (1u << N) - 1u;
+    if (t0 < 0) m &= m << -t0;
+    if (t0 + N > V) m &= (1u << (V - t0)) - 1u;
+    return m;
 }
 
 // Two values rounded to bf16 (nearest, ties to even), the first in the low half.
@@ -162,61 +171,69 @@ __device__ __forceinline__ void store_ids(void* row, int t0, int V, bool whole, 
     }
 }
 
-// A thread's part of a sequence, the same for all rows whose vectors lie alike: which of its ids were used, and their counts.
-template <int N> struct Used {
-    uint32_t bits;
-    float n[N];
-};
-template <int N>
-__device__ __forceinline__ Used<N> load_used(const ProcArgs& a, int b, int t0) {
-    Used<N> u;
-    u.bits = 0u;
-#pragma unroll
-    for (int e = 0; e < N; ++e) u.n[e] = 0.f;
-    if (a.penalties && a.seen != nullptr) {
-        u.bits = bits8(a.seen + static_cast<size_t>(b) * a.W, t0, 4 * a.W) & ((1u << N) - 1u);
-        if (u.bits != 0u) {
-#pragma unroll
-            for (int e = 0; e < N; ++e)
-                if ((u.bits >> e & 1u) && t0 + e < a.V) u.n[e] = static_cast<float>(__ldg(a.counts + static_cast<size_t>(b) * a.V + t0 + e));
-        }
+// One id of a packed vector, widened, and put back.
+template <int DT>
+__device__ __forceinline__ float id_of(const uint4& v, int e) {
+    if constexpr (DT == FSD_BF16) {
+        const uint32_t w = e < 4 ? (e < 2 ? v.x : v.y) : (e < 6 ? v.z : v.w);
+        return (e & 1) ? bf16_hi(w) : bf16_lo(w);
+    } else {
+        return __uint_as_float(e < 2 ? (e < 1 ? v.x : v.y) : (e < 3 ? v.z : v.w));
     }
-    return u;
+}
+template <int DT>
+__device__ __forceinline__ void set_id(uint4& v, int e, float x) {
+    if constexpr (DT == FSD_BF16) {
+        const uint32_t h = pack_bf16(x, 0.f), sel = (e & 1) ? 0x5410u : 0x3254u;        // h's low half over the word's upper or lower one
+        const int w = e >> 1;
+        v.x = w == 0 ? __byte_perm(v.x, h, sel) : v.x;
+        v.y = w == 1 ? __byte_perm(v.y, h, sel) : v.y;
+        v.z = w == 2 ? __byte_perm(v.z, h, sel) : v.z;
+        v.w = w == 3 ? __byte_perm(v.w, h, sel) : v.w;
+    } else {
+        const uint32_t u = __float_as_uint(x);
+        v.x = e == 0 ? u : v.x;
+        v.y = e == 1 ? u : v.y;
+        v.z = e == 2 ? u : v.z;
+        v.w = e == 3 ? u : v.w;
+    }
 }
 
-// The steps on one vector of a row.  special: which of its ids are in the span's bitmap; may: the row's mask.
-// bias_of: the entry of the list of biases that names an id, counted from 1 (0: none).
-template <int DT, class BiasOf>
-__device__ __forceinline__ void process_vec(const ProcArgs& a, const SeqParams& p, int b, int ctx, int t0, const Used<Logit<DT>::kPerVec>& u,
-                                            uint32_t special, uint32_t may, BiasOf bias_of, float (&x)[Logit<DT>::kPerVec]) {
+// The steps on one vector of a row, as it was read.  used: which of its ids the sequence has behind it, special: which of them
+// may be drafted or have a bias; may: the row's mask.  count_of: how often an id that is used was generated; bias_of: the entry of the
+// list of biases that names an id, counted from 1 (0: none).  The mask and the temperature go over the whole vector, the
+// rest over the ids that have it, one after another: there are few, and a step that goes over all eight because one of the
+// warp's ids has it made 115 instructions of 20 for each logit.
+template <int DT, class CountOf, class BiasOf>
+__device__ __forceinline__ uint4 process_vec(const ProcArgs& a, const SeqParams& p, int b, int ctx, int t0, uint4 v, uint32_t used, uint32_t special, uint32_t may,
+                                             CountOf count_of, BiasOf bias_of) {
     constexpr int N = Logit<DT>::kPerVec;
-    if ((u.bits | special) != 0u) {
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-            float n = u.n[e];
-            bool used = u.bits >> e & 1u;
-            if (special >> e & 1u) {
-                const int d = a.penalties ? drafted(a, b, ctx, t0 + e) : 0;
-                if (d > 0) {
-                    // (the counts are summed as whole numbers: together they may have more digits than a float)
-                    const int base = used ? __ldg(a.counts + static_cast<size_t>(b) * a.V + t0 + e) : 0;
-                    n = static_cast<float>(base + d);
-                    used = true;
-                }
-            }
-            if (used) x[e] = penalised(x[e], n, p);
-            if (special >> e & 1u) {
-                const int k = bias_of(t0 + e);
-                if (k > 0) x[e] = __fadd_rn(x[e], __ldg(a.bias_values + __ldg(a.bias_offsets + b) + k - 1));
-            }
-        }
-    }
-#pragma unroll
-    for (int e = 0; e < N; ++e) x[e] = (may >> e & 1u) ? x[e] : -INFINITY;
-    if (p.inv_temp != 1.f) {
+    constexpr uint32_t kAll = (1u << N) - 1u;
+    const uint4 raw = v;
+    if (p.inv_temp != 1.f || (may & kAll) != kAll) {
+        float x[N];
+        unpack_vec<DT>(v, x);
 #pragma unroll
         for (int e = 0; e < N; ++e) x[e] = __fmul_rn(x[e], p.inv_temp);
+        if ((may & kAll) != kAll) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) x[e] = (may >> e & 1u) ? x[e] : -INFINITY;
+        }
+        v = pack_vec<DT>(x);
     }
+    for (uint32_t todo = (used | special) & may; todo != 0u; todo &= todo - 1u) {
+        const int e = __ffs(static_cast<int>(todo)) - 1, t = t0 + e;
+        int n = (used >> e & 1u) ? count_of(t) : 0;
+        const int d = (special >> e & 1u) && a.penalties ? drafted(a, b, ctx, t) : 0;
+        float x = id_of<DT>(raw, e);
+        if ((used >> e & 1u) || d > 0) x = penalised(x, static_cast<float>(n + d), p);
+        if (special >> e & 1u) {
+            const int k = bias_of(t);
+            if (k > 0) x = __fadd_rn(x, __ldg(a.bias_values + __ldg(a.bias_offsets + b) + k - 1));
+        }
+        set_id<DT>(v, e, __fmul_rn(x, p.inv_temp));
+    }
+    return v;
 }
 
 // A block takes a span of the vocabulary, a vector a thread, for some rows of one sequence: the counts are read once for all
@@ -227,31 +244,61 @@ __global__ void __launch_bounds__(kProcThreads) fsd_process_kernel(const ProcArg
     constexpr int N = Logit<DT>::kPerVec, kSpan = kProcThreads * N + 32;
     using elem = typename Logit<DT>::elem;
     __shared__ Special<kSpan> special;
+    __shared__ int counts[kSpan];
     const int span = blockIdx.x % spans, group = blockIdx.x / spans % groups, b = blockIdx.x / spans / groups;
     const int lo = span * kProcThreads * N - 32;
+    const bool history = a.penalties && a.seen != nullptr;
+    if (history) {
+        const int first = lo < 0 ? 0 : lo;
+        for (int t = first + static_cast<int>(threadIdx.x) * 8; t < lo + kSpan && t < a.V; t += kProcThreads * 8)
+            for (uint32_t todo = bits8(a.seen + static_cast<size_t>(b) * a.W, t, 4 * a.W); todo != 0u; todo &= todo - 1u) {
+                const int u = t + __ffs(static_cast<int>(todo)) - 1;
+                if (u < a.V && u < lo + kSpan) counts[u - lo] = __ldg(a.counts + static_cast<size_t>(b) * a.V + u);
+            }
+    }
     find_special<kSpan>(a, b, lo, special);
     const SeqParams p = seq_params(a, b);
     const int all = a.rows[0] + a.rows[1], first = group * group_rows, last = first + group_rows < all ? first + group_rows : all;
-    Used<N> u;
-    int lies = -1;                                          // the alignment that u is for
-    for (int q = first; q < last; ++q) {
+
+    struct Row {                                            // a row's vector on the way
+        uint4 v;
+        uint32_t may;
+        int t0, ctx;
+        elem* out;
+        bool whole, alike;
+    };
+    const auto fetch = [&](int q) {
+        Row f;
         const int side = q >= a.rows[0], r = q - (side ? a.rows[0] : 0);
         const size_t at = (static_cast<size_t>(b) * a.rows[side] + r) * a.V;
         const elem* in = static_cast<const elem*>(a.in[side]) + at;
-        elem* out = static_cast<elem*>(a.out[side]) + at;
+        f.out = static_cast<elem*>(a.out[side]) + at;
         const int s = static_cast<int>(reinterpret_cast<uintptr_t>(in) % 16 / sizeof(elem));
-        const bool alike = (reinterpret_cast<uintptr_t>(in) ^ reinterpret_cast<uintptr_t>(out)) % 16 == 0;
-        const int t0 = (span * kProcThreads + static_cast<int>(threadIdx.x)) * N - s;
-        if (t0 >= a.V) continue;
-        const bool whole = t0 >= 0 && t0 + N <= a.V;
-        float x[N];
-        load_ids<DT>(in, t0, a.V, whole, x);
-        const int ctx = context_row(a, b, side, r);
-        const uint32_t may = a.allowed != nullptr ? bits8(a.allowed + (static_cast<size_t>(b) * (a.P + 1) + ctx) * a.W, t0, 4 * a.W) : 0xffu;
-        if (s != lies) { u = load_used<N>(a, b, t0); lies = s; }
-        const uint32_t sp = special.any ? bits8(special.bits, t0 - lo, sizeof(special.bits)) & ((1u << N) - 1u) : 0u;
-        process_vec<DT>(a, p, b, ctx, t0, u, sp, may, [&](int t) { return a.bias_offsets != nullptr ? special.bias[t - lo] : 0; }, x);
-        store_ids<DT>(out, t0, a.V, whole && alike, pack_vec<DT>(x));
+        f.alike = (reinterpret_cast<uintptr_t>(in) ^ reinterpret_cast<uintptr_t>(f.out)) % 16 == 0;
+        f.t0 = (span * kProcThreads + static_cast<int>(threadIdx.x)) * N - s;
+        f.whole = f.t0 >= 0 && f.t0 + N <= a.V;
+        f.ctx = context_row(a, b, side, r);
+        f.may = 0xffu;
+        f.v = make_uint4(0u, 0u, 0u, 0u);
+        if (f.t0 < a.V) {
+            f.v = load_ids<DT>(in, f.t0, a.V, f.whole);
+            if (!f.whole) f.may = ids_of<N>(f.t0, a.V);
+            if (a.allowed != nullptr) f.may &= bits8(a.allowed + (static_cast<size_t>(b) * (a.P + 1) + f.ctx) * a.W, f.t0, 4 * a.W);
+        }
+        return f;
+    };
+    uint32_t used = 0u;
+    int used_at = INT_MIN;                                  // the id that `used` starts at
+    Row next = fetch(first);
+    for (int q = first; q < last; ++q) {
+        const Row f = next;
+        if (q + 1 < last) next = fetch(q + 1);
+        if (f.t0 >= a.V) continue;
+        if (history && f.t0 != used_at) { used = bits8(a.seen + static_cast<size_t>(b) * a.W, f.t0, 4 * a.W) & ((1u << N) - 1u); used_at = f.t0; }
+        const uint32_t sp = special.any ? bits8(special.bits, f.t0 - lo, sizeof(special.bits)) & ((1u << N) - 1u) : 0u;
+        const uint4 y = process_vec<DT>(a, p, b, f.ctx, f.t0, f.v, used, sp, f.may, [&](int t) { return counts[t - lo]; },
+                                        [&](int t) { return a.bias_offsets != nullptr ? special.bias[t - lo] : 0; });
+        store_ids<DT>(f.out, f.t0, a.V, f.whole && f.alike, y);
     }
 }
 

@@ -5,6 +5,7 @@
 // whole in a flat row of 150000: sums are in double precision, and whether two programs agree never hangs on their order.
 #pragma once
 
+#include <cuda_bf16.h>
 #include <type_traits>
 
 #include "fsd_process.cuh"
@@ -59,14 +60,29 @@ __device__ __forceinline__ long long ties_below(double above, double w, double g
     return j < 1.0 ? 1 : j > static_cast<double>(V) ? V : static_cast<long long>(j);
 }
 
-// The smallest key whose value is no further below the largest, `most` with key `top`, than ln(min_p).
+// (Out of line: the places that need it are many and reached seldom.)
+__device__ __noinline__ double exp_d(double x) { return exp(x); }
+
+// The smallest key whose value is no further below the largest, `most` with key `top`, than ln(min_p).  A whole warp.
 template <int DT>
-__device__ __forceinline__ uint32_t min_p_key(float min_p, uint32_t top, double most) {
+__device__ __noinline__ uint32_t min_p_key(float min_p, uint32_t top, double most) {
     const double far = log(static_cast<double>(min_p < 1.f ? min_p : 1.f));
+    const uint32_t lane = threadIdx.x & 31;
     uint32_t lo = key_of_value<DT>(-INFINITY), hi = top;        // hi always is, lo never
     while (hi - lo > 1u) {
-        const uint32_t mid = lo + (hi - lo) / 2u;
-        if (static_cast<double>(value_of<DT>(mid)) - most >= far) hi = mid; else lo = mid;
+        const uint32_t step = (hi - lo) / 33u + 1u;
+        const auto at = [&](uint32_t k) { return step * k < hi - lo ? lo + step * k : hi; };
+        const uint32_t is = __ballot_sync(0xffffffffu, static_cast<double>(value_of<DT>(at(lane + 1u))) - most >= far) | 1u << 31;
+        const uint32_t k = __ffs(static_cast<int>(is)) - 1;     // (where no lane below the last is, the last may not be either: hi stays)
+        const bool last = __shfl_sync(0xffffffffu, static_cast<double>(value_of<DT>(at(32u))) - most >= far, 0);
+        const uint32_t old_lo = lo, old_hi = hi;
+        const auto from = [&](uint32_t j) { return step * j < old_hi - old_lo ? old_lo + step * j : old_hi; };
+        if (k == 31u && !last) {
+            lo = from(32u);
+        } else {
+            lo = k == 0u ? old_lo : from(k);
+            hi = from(k + 1u);
+        }
     }
     return hi;
 }
@@ -82,7 +98,7 @@ struct Cut {
     int until;
 };
 template <int DT, class Total, class Largest>
-__device__ Cut find_cut(const LogitWord<DT>* row, int n, int first, int V, const CutParams& c, Total total, Largest largest) {
+__device__ __noinline__ Cut find_cut(const LogitWord<DT>* row, int n, int first, int V, const CutParams& c, Total total, Largest largest) {
     const int tid = threadIdx.x, step = blockDim.x;
     uint32_t top = 0u;
     for (int i = tid; i < n; i += step) {
@@ -94,7 +110,7 @@ __device__ Cut find_cut(const LogitWord<DT>* row, int n, int first, int V, const
     top = largest(top);
     if (top >= key_of_value<DT>(INFINITY) || top <= key_of_value<DT>(-INFINITY)) return {false, 0u, 0};
     const double most = value_of<DT>(top);
-    const auto weight = [&](uint32_t key) { return exp(static_cast<double>(value_of<DT>(key)) - most); };
+    const auto weight = [&](uint32_t key) { return exp_d(static_cast<double>(value_of<DT>(key)) - most); };
     // tokens with keys of at least t: how many, and (with weights) what those above `over` weigh
     const auto at_least = [&](uint32_t t, uint32_t over, bool weights) {
         CountAndWeight v = {0, 0.0};
@@ -296,7 +312,7 @@ __device__ void solve_bins(const uint32_t* hist, CutShared& s, const CutParams& 
         const int bin = kBins - 1 - (tid * kBinsEach + j);
         n[j] = bin >= 0 ? hist[bin] : 0u;
         w[j] = 0.0;
-        if (n[j] != 0u && one_value(bin)) w[j] = exp(bin_value<DT>(bin));
+        if (n[j] != 0u && one_value(bin)) w[j] = exp_d(bin_value<DT>(bin));
         mine.n += n[j];
         mine.w += bin == kBinTinyPos ? tiny : n[j] * w[j];
     }
@@ -388,12 +404,13 @@ __device__ void solve_bins(const uint32_t* hist, CutShared& s, const CutParams& 
             if (s.work.ties >= hist[k_bin]) s.work.ties = V;
         }
         __syncthreads();
-        if (tid == 0 && c.m) {
-            const uint32_t t = min_p_key<DT>(c.min_p, top, most);
-            if (t > s.work.key) { s.work.key = t; s.work.ties = V; }
+        if (tid < 32) {
+            const uint32_t t = c.m ? min_p_key<DT>(c.min_p, top, most) : 0u;
+            if (tid == 0 && t > s.work.key) { s.work.key = t; s.work.ties = V; }
+            if (tid == 0 && s.work.key == 0u) s.work.kind = kCutNone;
         }
-        if (tid == 0 && s.work.key == 0u) s.work.kind = kCutNone;
     } else {
+        const uint32_t t = tid < 32 && c.m && !cut_k && !c.p ? min_p_key<DT>(c.min_p, top, most) : 0u;
         if (tid == 0) {
             s.found[3] = p_bin;
             if (cut_k) {
@@ -403,7 +420,7 @@ __device__ void solve_bins(const uint32_t* hist, CutShared& s, const CutParams& 
                 s.work.kind = kCutRefineP;
                 s.work.key = bin_prefix(p_bin);
             } else if (c.m) {
-                s.work.key = min_p_key<DT>(c.min_p, top, most);
+                s.work.key = t;
             } else {
                 s.work.kind = kCutNone;                     // (fewer tokens than top_k)
             }
@@ -488,9 +505,9 @@ __device__ __forceinline__ int next_bin(const uint32_t* hist, CutShared& s, int 
     return found == kBins ? -1 : found;
 }
 
-__device__ __forceinline__ void at_least_min_p(CutShared& s, const CutParams& c, int V, uint32_t top) {       // one thread
+__device__ __forceinline__ void at_least_min_p(CutShared& s, const CutParams& c, int V, uint32_t top) {       // one warp
     const uint32_t t = min_p_key<FSD_F32>(c.min_p, top, value_of<FSD_F32>(top));
-    if (t > s.work.key) { s.work.key = t; s.work.ties = V; }
+    if (threadIdx.x == 0 && t > s.work.key) { s.work.key = t; s.work.ties = V; }
 }
 
 // fp32: from the bins of the cuts to the cuts.
@@ -515,9 +532,11 @@ __device__ CutResult refine(const RowSlice<FSD_F32>& row, const uint32_t* hist, 
                     if (shift == 0) s.work.over = s.work.ties >= n;            // whether all that are equal are kept
                 }
                 __syncthreads();
-                if (tid == 0 && shift == 0 && !c.p) {
-                    s.work.kind = kCutDone;
-                    if (s.work.over) s.work.ties = V;
+                if (tid < 32 && shift == 0 && !c.p) {
+                    if (tid == 0) {
+                        s.work.kind = kCutDone;
+                        if (s.work.over) s.work.ties = V;
+                    }
                     if (c.m) at_least_min_p(s, c, V, top);
                 }
             }
@@ -529,7 +548,7 @@ __device__ CutResult refine(const RowSlice<FSD_F32>& row, const uint32_t* hist, 
     const uint32_t over = cut_k ? res.key : 0u;
     const long long k_ties = cut_k ? res.ties : 0;
     const bool all_of_k = cut_k && res.over;
-    const double of_ties = cut_k ? static_cast<double>(k_ties) * exp(static_cast<double>(value_of<FSD_F32>(over)) - most) : 0.0;
+    const double of_ties = cut_k ? static_cast<double>(k_ties) * exp_d(static_cast<double>(value_of<FSD_F32>(over)) - most) : 0.0;
     if (cut_k) {
         if (rank == 0 && tid == 0) s.work = {kCutRefineP, bin_prefix(p_bin), 0, 0u};
         res = tell_result(s, cluster, rank, blocks, turn);
@@ -544,7 +563,7 @@ __device__ CutResult refine(const RowSlice<FSD_F32>& row, const uint32_t* hist, 
         if (rank == 0) {
             double above = 0.0, rest = 0.0;
             for (int k = 0; k < blocks; ++k) { above += s.above[k]; rest += s.rest[k]; }
-            const double unit = exp(static_cast<double>(value_of<FSD_F32>(prefix << 16 | 0xffffu)) - most) / kFixed;
+            const double unit = exp_d(static_cast<double>(value_of<FSD_F32>(prefix << 16 | 0xffffu)) - most) / kFixed;
             CountAndWeight all;
             const int bin = 255 - tid;
             const double w = tid < 256 ? static_cast<double>(s.sub_w[bin]) * unit : 0.0;
@@ -592,7 +611,7 @@ __device__ CutResult refine(const RowSlice<FSD_F32>& row, const uint32_t* hist, 
             const int bin = 255 - tid;
             const uint32_t key = prefix << 8 | static_cast<uint32_t>(bin);
             const long long n = tid < 256 ? s.sub_n[bin] : 0;
-            const double w = n != 0 ? exp(static_cast<double>(value_of<FSD_F32>(key)) - most) : 0.0;
+            const double w = n != 0 ? exp_d(static_cast<double>(value_of<FSD_F32>(key)) - most) : 0.0;
             const CountAndWeight before = scan_threads({n, static_cast<double>(n) * w}, s.scratch, all);
             if (tid == 0) s.found[2] = 256;
             __syncthreads();
@@ -607,7 +626,7 @@ __device__ CutResult refine(const RowSlice<FSD_F32>& row, const uint32_t* hist, 
         }
     }
     if (res.kind != kCutByBits && (res.kind == kCutRefineK || c.m)) {
-        if (rank == 0 && tid == 0 && c.m) at_least_min_p(s, c, V, top);
+        if (rank == 0 && tid < 32 && c.m) at_least_min_p(s, c, V, top);
         res = tell_result(s, cluster, rank, blocks, turn);
     }
     return res;
@@ -624,9 +643,57 @@ __device__ __forceinline__ void words_of(const uint4& v, uint32_t (&bits)[Logit<
     }
 }
 
+// One value into the bins; those that share a bin with others of their size are weighed.
+__device__ __noinline__ double count_value(uint32_t bits, uint32_t* hist) {
+    if (bits == 0xff800000u) return 0.0;
+    const uint32_t mag = bits >> 16 & 0x7fffu, u = (mag < kMagLo ? kMagLo : mag > kMagHi ? kMagHi : mag) - kMagLo;
+    int bin = static_cast<int>(u ^ static_cast<uint32_t>(static_cast<int>(bits) >> 31)) + kHalfBins;
+    if ((bits & 0x7fffffffu) > 0x7f800000u) bin = kBinOver;
+    atomicAdd(&hist[bin], 1u);
+    return u != 0u ? 0.0 : (bits & 0x7fffffffu) == 0u ? 1.0 : exp(static_cast<double>(__uint_as_float(bits)));
+}
+// A vector of values into the bins; returns what is weighed.  bf16: two at a time, in halves of a word.
+template <int DT>
+__device__ __forceinline__ double count_vec(const uint4& v, uint32_t* hist) {
+    double tiny = 0.0;
+    if constexpr (DT == FSD_BF16) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        uint32_t bin[4], lowest = 0xffffffffu, highest = 0u;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t m = __vminu2(__vmaxu2(w[k] & 0x7fff7fffu, kMagLo * 0x10001u), kMagHi * 0x10001u);
+            lowest = __vminu2(lowest, m);
+            highest = __vmaxu2(highest, m);
+            uint32_t sign;                                  // each half's sign in all of its bits
+            asm("prmt.b32 %0, %1, 0, 0xbb99;" : "=r"(sign) : "r"(w[k]));
+            bin[k] = (m - kMagLo * 0x10001u) ^ sign;
+        }
+        if ((lowest & 0xffffu) == kMagLo || lowest >> 16 == kMagLo || (highest & 0xffffu) == kMagHi || highest >> 16 == kMagHi) {
+#pragma unroll 1
+            for (int e = 0; e < 8; ++e) tiny += count_value(__float_as_uint(id_of<DT>(v, e)), hist);
+        } else {
+            uint32_t* mid = hist + kHalfBins;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                atomicAdd(mid + static_cast<int16_t>(bin[k]), 1u);
+                atomicAdd(mid + (static_cast<int>(bin[k]) >> 16), 1u);
+            }
+        }
+    } else {
+        const uint32_t bits[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t mag = bits[e] >> 16 & 0x7fffu;
+            if (mag <= kMagLo || mag >= kMagHi) tiny += count_value(bits[e], hist);
+            else atomicAdd(&hist[static_cast<int>((mag - kMagLo) ^ static_cast<uint32_t>(static_cast<int>(bits[e]) >> 31)) + kHalfBins], 1u);
+        }
+    }
+    return tiny;
+}
+
 // raw: the rows are processed already.
 template <int DT>
-__global__ void __launch_bounds__(kRowThreads) fsd_cut_kernel(const ProcArgs a, int slice, bool raw) {
+__global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_kernel(const ProcArgs a, int slice, bool raw) {
     constexpr int N = Logit<DT>::kPerVec;
     using elem = typename Logit<DT>::elem;
     extern __shared__ uint4 on_chip[];
@@ -668,7 +735,7 @@ __global__ void __launch_bounds__(kRowThreads) fsd_cut_kernel(const ProcArgs a, 
         }
     }
     __syncthreads();
-    const bool any_special = s.any_special != 0;
+    const bool any_special = s.any_special != 0, history = a.penalties && a.seen != nullptr;
 
     // the slice: read, processed, counted, kept
     double tiny = 0.0;
@@ -677,37 +744,25 @@ __global__ void __launch_bounds__(kRowThreads) fsd_cut_kernel(const ProcArgs a, 
     for (int i = tid; i < row.n; i += kRowThreads) {
         const int t0 = row.first + i * N;
         const bool whole = t0 >= 0 && t0 + N <= a.V;
-        float x[N];
-        load_ids<DT>(in, t0, a.V, whole, x);
+        uint4 v = load_ids<DT>(in, t0, a.V, whole);
         if (!raw) {
-            const uint32_t may = a.allowed != nullptr ? bits8(a.allowed + (static_cast<size_t>(b) * (a.P + 1) + ctx) * a.W, t0, 4 * a.W) : 0xffu;
-            const Used<N> u = load_used<N>(a, b, t0);
+            uint32_t may = a.allowed != nullptr ? bits8(a.allowed + (static_cast<size_t>(b) * (a.P + 1) + ctx) * a.W, t0, 4 * a.W) : 0xffu;
+            if (!whole) may &= ids_of<N>(t0, a.V);              // (what is not in the row counts as masked)
+            const uint32_t used = history ? bits8(a.seen + static_cast<size_t>(b) * a.W, t0, 4 * a.W) & ((1u << N) - 1u) : 0u;
             const uint32_t sp = any_special && (s.special[i >> coarse >> 5] >> (i >> coarse & 31) & 1u) ? (1u << N) - 1u : 0u;
-            process_vec<DT>(a, p, b, ctx, t0, u, sp, may, [](int) { return 0; }, x);
+            v = process_vec<DT>(a, p, b, ctx, t0, v, used, sp, may, [&](int t) { return __ldg(a.counts + static_cast<size_t>(b) * a.V + t); }, [](int) { return 0; });
         }
-        const uint4 v = pack_vec<DT>(x);
         if (!cutting) {
             store_ids<DT>(out, t0, a.V, whole && alike, v);
             continue;
         }
-        uint32_t bits[N];
-        words_of<DT>(v, bits);
+        tiny += count_vec<DT>(v, hist);
+        if constexpr (DT == FSD_F32) {
+            const uint32_t bits[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            if (!whole && (t0 + e < 0 || t0 + e >= a.V)) { bits[e] = 0xff800000u; continue; }
-            if (bits[e] == 0xff800000u) continue;
-            const uint32_t mag = bits[e] >> 16 & 0x7fffu;
-            uint32_t u = (mag < kMagLo ? kMagLo : mag > kMagHi ? kMagHi : mag) - kMagLo;
-            int bin = static_cast<int>(u ^ static_cast<uint32_t>(static_cast<int>(bits[e]) >> 31)) + kHalfBins;
-            if (u == 0u) tiny += exp(static_cast<double>(__uint_as_float(bits[e])));
-            if ((bits[e] & 0x7fffffffu) > 0x7f800000u) bin = kBinOver;
-            atomicAdd(&hist[bin], 1u);
-            if constexpr (DT == FSD_F32) { const uint32_t k = key_of<DT>(bits[e]); top = top > k ? top : k; }
+            for (int e = 0; e < 4; ++e) { const uint32_t k = key_of<DT>(bits[e]); top = top > k ? top : k; }
         }
-        if (whole) row.vecs[i] = v;
-        else if constexpr (DT == FSD_BF16)
-            row.vecs[i] = make_uint4(bits[0] >> 16 | bits[1], bits[2] >> 16 | bits[3], bits[4] >> 16 | bits[5], bits[6] >> 16 | bits[7]);
-        else row.vecs[i] = make_uint4(bits[0], bits[1], bits[2], bits[3]);
+        row.vecs[i] = v;
     }
     if (!cutting) { cluster_wait(); return; }               // (the whole cluster: it is the sequence that asks)
 
@@ -760,8 +815,8 @@ __global__ void __launch_bounds__(kRowThreads) fsd_cut_kernel(const ProcArgs a, 
         };
         const Cut cut = find_cut<DT>(reinterpret_cast<const LogitWord<DT>*>(row.vecs), row.n * N, row.first, a.V, c, total, largest);
         key = cut.key;
-        until = cut.until;
         keep_all = !cut.any;
+        if (cut.any) until = cut.until;
     }
     const long long ties = res.kind == kCutDone ? res.ties : a.V;
     const float value = value_of<DT>(key);
@@ -785,6 +840,31 @@ __global__ void __launch_bounds__(kRowThreads) fsd_cut_kernel(const ProcArgs a, 
         cluster_barrier();
         for (int k = 0; k < rank; ++k) before += s.equal[k];
         before += ahead;
+    }
+    if (ties >= a.V && until >= a.V) {                      // all that are equal to the cut are kept
+        for (int i = tid; i < row.n; i += kRowThreads) {
+            uint4 v = row.vecs[i];
+            if (!keep_all) {
+                if constexpr (DT == FSD_BF16) {
+                    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                    const __nv_bfloat162 cut2 = __bfloat162bfloat162(__float2bfloat16_rn(value));       // (value is one of bf16)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t keep = __hge2_mask(*reinterpret_cast<const __nv_bfloat162*>(&w[k]), cut2);
+                        w[k] = (w[k] & keep) | (0xff80ff80u & ~keep);
+                    }
+                    v = make_uint4(w[0], w[1], w[2], w[3]);
+                } else {
+                    v.x = __uint_as_float(v.x) >= value ? v.x : 0xff800000u;
+                    v.y = __uint_as_float(v.y) >= value ? v.y : 0xff800000u;
+                    v.z = __uint_as_float(v.z) >= value ? v.z : 0xff800000u;
+                    v.w = __uint_as_float(v.w) >= value ? v.w : 0xff800000u;
+                }
+            }
+            const int t0 = row.first + i * N;
+            store_ids<DT>(out, t0, a.V, t0 >= 0 && t0 + N <= a.V && alike, v);
+        }
+        return;
     }
     for (int i0 = w0; i0 < w1; i0 += 32) {
         const int i = i0 + lane;
@@ -810,7 +890,7 @@ __global__ void __launch_bounds__(kRowThreads) fsd_cut_kernel(const ProcArgs a, 
         }
         if (i >= w1) continue;
         const int t0 = row.first + i * N;
-        if (!keep_all) {
+        {
             uint32_t out_bits[N];
 #pragma unroll
             for (int e = 0; e < N; ++e) {
