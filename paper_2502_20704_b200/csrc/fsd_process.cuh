@@ -82,20 +82,26 @@ __device__ __forceinline__ uint32_t bits8(const void* words, int t0, int bytes) 
     return w & 0xffu;
 }
 
-// Vocabulary ids that need more than the sequence's counts in a block's span: a bitmap of the ids with a bias or among the
-// drafted tokens, and for each id the last entry of the list of biases that names it (counted from 1; 0: none).
-template <int SPAN> struct Special {
+// The ids of a block's span that need more than the mask and the temperature: used ones, drafted ones and those with a
+// bias.  A bitmap of them and a list in no order, how often each was generated, and for each the last entry of the list of
+// biases that names it (counted from 1; 0: none).
+template <int SPAN> struct Sparse {
+    uint32_t drafted[(SPAN + 31) / 32 + 1];                // drafted or biased: to be looked at again in each row
     uint32_t bits[(SPAN + 31) / 32 + 1];
     int bias[SPAN];
-    int any;
+    int counts[SPAN];
+    uint16_t list[SPAN];
+    int n;
 };
 // All of the block's threads.  lo: the span's first id, a multiple of 32 (it may be negative).  Ends with a barrier.
 template <int SPAN>
-__device__ void find_special(const ProcArgs& a, int b, int lo, Special<SPAN>& s) {
+__device__ __forceinline__ void find_sparse(const ProcArgs& a, int b, int lo, Sparse<SPAN>& s) {
+    static_assert(SPAN % 32 == 0, "whole words");
     const int b0 = a.bias_offsets != nullptr ? __ldg(a.bias_offsets + b) : 0, b1 = a.bias_offsets != nullptr ? __ldg(a.bias_offsets + b + 1) : 0;
     const int drafts = a.penalties && a.tokens != nullptr ? a.P : 0;
-    if (threadIdx.x == 0) s.any = 0;
-    for (int i = threadIdx.x; i < (SPAN + 31) / 32 + 1; i += blockDim.x) s.bits[i] = 0u;
+    const bool history = a.penalties && a.seen != nullptr;
+    if (threadIdx.x == 0) s.n = 0;
+    for (int i = threadIdx.x; i < SPAN / 32 + 1; i += blockDim.x) { s.drafted[i] = 0u; s.bits[i] = 0u; }
     if (a.bias_offsets != nullptr)
         for (int i = threadIdx.x; i < SPAN; i += blockDim.x) s.bias[i] = 0;
     __syncthreads();
@@ -103,15 +109,29 @@ __device__ void find_special(const ProcArgs& a, int b, int lo, Special<SPAN>& s)
         const int t = __ldg(a.bias_tokens + i), k = t - lo;
         if (t >= 0 && t < a.V && k >= 0 && k < SPAN) {
             atomicMax(&s.bias[k], i - b0 + 1);
-            atomicOr(&s.bits[k >> 5], 1u << (k & 31));
-            s.any = 1;
+            atomicOr(&s.drafted[k >> 5], 1u << (k & 31));
         }
     }
     for (int j = threadIdx.x; j < drafts; j += blockDim.x) {
         const int t = __ldg(a.tokens + static_cast<size_t>(b) * a.P + j), k = t - lo;
-        if (t >= 0 && t < a.V && k >= 0 && k < SPAN) {
-            atomicOr(&s.bits[k >> 5], 1u << (k & 31));
-            s.any = 1;
+        if (t >= 0 && t < a.V && k >= 0 && k < SPAN) atomicOr(&s.drafted[k >> 5], 1u << (k & 31));
+    }
+    if (drafts > 0 || b1 > b0) __syncthreads();
+    // eight ids a thread
+    for (int k = static_cast<int>(threadIdx.x) * 8; k < SPAN; k += static_cast<int>(blockDim.x) * 8) {
+        const int t = lo + k;
+        if (t < 0 || t >= a.V) continue;
+        uint32_t used = history ? bits8(a.seen + static_cast<size_t>(b) * a.W, t, 4 * a.W) : 0u;
+        if (t + 8 > a.V) used &= (1u << (a.V - t)) - 1u;
+        const uint32_t any = used | (s.drafted[k >> 5] >> (k & 31) & 0xffu);
+        if (any == 0u) continue;
+        reinterpret_cast<uint8_t*>(s.bits)[k >> 3] = static_cast<uint8_t>(any);
+        int at = atomicAdd(&s.n, __popc(any));
+        for (uint32_t todo = any; todo != 0u; todo &= todo - 1u) {
+            const int e = __ffs(static_cast<int>(todo)) - 1;
+            s.list[at++] = static_cast<uint16_t>(k + e);
+            // (a token that is used has a count of its own, 0 if it is only in the prompt; -1: not used)
+            s.counts[k + e] = (used >> e & 1u) ? __ldg(a.counts + static_cast<size_t>(b) * a.V + t + e) : -1;
         }
     }
     __syncthreads();
@@ -171,99 +191,80 @@ __device__ __forceinline__ void store_ids(void* row, int t0, int V, bool whole, 
     }
 }
 
-// One id of a packed vector, widened, and put back.
+// One id of a row, widened, and put back.
 template <int DT>
-__device__ __forceinline__ float id_of(const uint4& v, int e) {
-    if constexpr (DT == FSD_BF16) {
-        const uint32_t w = e < 4 ? (e < 2 ? v.x : v.y) : (e < 6 ? v.z : v.w);
-        return (e & 1) ? bf16_hi(w) : bf16_lo(w);
-    } else {
-        return __uint_as_float(e < 2 ? (e < 1 ? v.x : v.y) : (e < 3 ? v.z : v.w));
-    }
+__device__ __forceinline__ float read_id(const void* row, int t) {
+    if constexpr (DT == FSD_BF16) return __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(row)[t]) << 16);
+    else return static_cast<const float*>(row)[t];
 }
 template <int DT>
-__device__ __forceinline__ void set_id(uint4& v, int e, float x) {
-    if constexpr (DT == FSD_BF16) {
-        const uint32_t h = pack_bf16(x, 0.f), sel = (e & 1) ? 0x5410u : 0x3254u;        // h's low half over the word's upper or lower one
-        const int w = e >> 1;
-        v.x = w == 0 ? __byte_perm(v.x, h, sel) : v.x;
-        v.y = w == 1 ? __byte_perm(v.y, h, sel) : v.y;
-        v.z = w == 2 ? __byte_perm(v.z, h, sel) : v.z;
-        v.w = w == 3 ? __byte_perm(v.w, h, sel) : v.w;
-    } else {
-        const uint32_t u = __float_as_uint(x);
-        v.x = e == 0 ? u : v.x;
-        v.y = e == 1 ? u : v.y;
-        v.z = e == 2 ? u : v.z;
-        v.w = e == 3 ? u : v.w;
-    }
+__device__ __forceinline__ void write_id(void* row, int t, float x) {
+    if constexpr (DT == FSD_BF16) static_cast<uint16_t*>(row)[t] = static_cast<uint16_t>(pack_bf16(x, 0.f));
+    else static_cast<float*>(row)[t] = x;
 }
 
-// The steps on one vector of a row, as it was read.  used: which of its ids the sequence has behind it, special: which of them
-// may be drafted or have a bias; may: the row's mask.  count_of: how often an id that is used was generated; bias_of: the entry of the
-// list of biases that names an id, counted from 1 (0: none).  The mask and the temperature go over the whole vector, the
-// rest over the ids that have it, one after another: there are few, and a step that goes over all eight because one of the
-// warp's ids has it made 115 instructions of 20 for each logit.
-template <int DT, class CountOf, class BiasOf>
-__device__ __forceinline__ uint4 process_vec(const ProcArgs& a, const SeqParams& p, int b, int ctx, int t0, uint4 v, uint32_t used, uint32_t special, uint32_t may,
-                                             CountOf count_of, BiasOf bias_of) {
+// The mask and the temperature on one vector of a row.
+template <int DT>
+__device__ __forceinline__ uint4 process_vec(uint4 v, uint32_t may, float inv_temp) {
     constexpr int N = Logit<DT>::kPerVec;
     constexpr uint32_t kAll = (1u << N) - 1u;
-    const uint4 raw = v;
-    if (p.inv_temp != 1.f || (may & kAll) != kAll) {
-        float x[N];
-        unpack_vec<DT>(v, x);
+    if (inv_temp == 1.f && (may & kAll) == kAll) return v;
+    float x[N];
+    unpack_vec<DT>(v, x);
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = __fmul_rn(x[e], p.inv_temp);
-        if ((may & kAll) != kAll) {
+    for (int e = 0; e < N; ++e) x[e] = __fmul_rn(x[e], inv_temp);
+    if ((may & kAll) != kAll) {
 #pragma unroll
-            for (int e = 0; e < N; ++e) x[e] = (may >> e & 1u) ? x[e] : -INFINITY;
-        }
-        v = pack_vec<DT>(x);
+        for (int e = 0; e < N; ++e) x[e] = (may >> e & 1u) ? x[e] : -INFINITY;
     }
-    for (uint32_t todo = (used | special) & may; todo != 0u; todo &= todo - 1u) {
-        const int e = __ffs(static_cast<int>(todo)) - 1, t = t0 + e;
-        int n = (used >> e & 1u) ? count_of(t) : 0;
-        const int d = (special >> e & 1u) && a.penalties ? drafted(a, b, ctx, t) : 0;
-        float x = id_of<DT>(raw, e);
-        if ((used >> e & 1u) || d > 0) x = penalised(x, static_cast<float>(n + d), p);
-        if (special >> e & 1u) {
-            const int k = bias_of(t);
-            if (k > 0) x = __fadd_rn(x, __ldg(a.bias_values + __ldg(a.bias_offsets + b) + k - 1));
-        }
-        set_id<DT>(v, e, __fmul_rn(x, p.inv_temp));
-    }
-    return v;
+    return pack_vec<DT>(x);
+}
+// All steps but the mask on one logit.  n: how often its token was generated, -1: it is not behind the sequence; d: how often it is drafted.
+__device__ __forceinline__ float process_id(float x, int n, int d, float bias, bool biased, const SeqParams& p) {
+    if (n >= 0 || d > 0) x = penalised(x, static_cast<float>((n > 0 ? n : 0) + d), p);
+    if (biased) x = __fadd_rn(x, bias);
+    return __fmul_rn(x, p.inv_temp);
 }
 
-// A block takes a span of the vocabulary, a vector a thread, for some rows of one sequence: the counts are read once for all
-// of them.  Vectors are aligned in memory and not in the vocabulary: where a row starts s ids behind a 16-byte boundary, vector v
+// Bits as masks of a vector's halves or words.
+template <int DT>
+__device__ __forceinline__ uint4 spread_bits(uint32_t bits) {
+    if constexpr (DT == FSD_BF16) {
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = (bits >> (2 * k) & 1u) * 0xffffu | (bits >> (2 * k + 1) & 1u) * 0xffff0000u;
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+        return make_uint4((bits & 1u) * 0xffffffffu, (bits >> 1 & 1u) * 0xffffffffu, (bits >> 2 & 1u) * 0xffffffffu, (bits >> 3 & 1u) * 0xffffffffu);
+    }
+}
+__device__ __forceinline__ uint4 merge(const uint4& a, const uint4& b, const uint4& of_b) {
+    return make_uint4((a.x & ~of_b.x) | (b.x & of_b.x), (a.y & ~of_b.y) | (b.y & of_b.y), (a.z & ~of_b.z) | (b.z & of_b.z), (a.w & ~of_b.w) | (b.w & of_b.w));
+}
+
+// A block takes a span of the vocabulary, a vector a thread, for some rows of one sequence.  First the mask and the temperature,
+// a vector at a time, which leave the sparse ids as they were read; then these, one id a thread, all rows' in one list: few of a
+// vector's ids are in it, but of a warp's 256 some always are, and a loop over a vector's own took 50 instructions a logit
+// where this takes 10.  Counts and biases are looked up once for all rows.
+// Vectors are aligned in memory and not in the vocabulary: where a row starts s ids behind a 16-byte boundary, vector v
 // covers ids N v - s and on, and a row whose output lies differently is stored an id at a time.
 template <int DT>
 __global__ void __launch_bounds__(kProcThreads) fsd_process_kernel(const ProcArgs a, int spans, int groups, int group_rows) {
-    constexpr int N = Logit<DT>::kPerVec, kSpan = kProcThreads * N + 32;
+    constexpr int N = Logit<DT>::kPerVec, kIds = kProcThreads * N, kSpan = kIds + 32;
     using elem = typename Logit<DT>::elem;
-    __shared__ Special<kSpan> special;
-    __shared__ int counts[kSpan];
+    __shared__ Sparse<kSpan> sparse;
     const int span = blockIdx.x % spans, group = blockIdx.x / spans % groups, b = blockIdx.x / spans / groups;
-    const int lo = span * kProcThreads * N - 32;
-    const bool history = a.penalties && a.seen != nullptr;
-    if (history) {
-        const int first = lo < 0 ? 0 : lo;
-        for (int t = first + static_cast<int>(threadIdx.x) * 8; t < lo + kSpan && t < a.V; t += kProcThreads * 8)
-            for (uint32_t todo = bits8(a.seen + static_cast<size_t>(b) * a.W, t, 4 * a.W); todo != 0u; todo &= todo - 1u) {
-                const int u = t + __ffs(static_cast<int>(todo)) - 1;
-                if (u < a.V && u < lo + kSpan) counts[u - lo] = __ldg(a.counts + static_cast<size_t>(b) * a.V + u);
-            }
-    }
-    find_special<kSpan>(a, b, lo, special);
+    const int lo = span * kIds - 32;
+    const bool some = a.penalties || a.bias_offsets != nullptr;
+    if (some) find_sparse<kSpan>(a, b, lo, sparse);
+    const int n_sparse = some ? sparse.n : 0;
     const SeqParams p = seq_params(a, b);
     const int all = a.rows[0] + a.rows[1], first = group * group_rows, last = first + group_rows < all ? first + group_rows : all;
 
     struct Row {                                            // a row's vector on the way
         uint4 v;
         uint32_t may;
-        int t0, ctx;
+        int t0;
         elem* out;
         bool whole, alike;
     };
@@ -277,28 +278,70 @@ __global__ void __launch_bounds__(kProcThreads) fsd_process_kernel(const ProcArg
         f.alike = (reinterpret_cast<uintptr_t>(in) ^ reinterpret_cast<uintptr_t>(f.out)) % 16 == 0;
         f.t0 = (span * kProcThreads + static_cast<int>(threadIdx.x)) * N - s;
         f.whole = f.t0 >= 0 && f.t0 + N <= a.V;
-        f.ctx = context_row(a, b, side, r);
         f.may = 0xffu;
         f.v = make_uint4(0u, 0u, 0u, 0u);
         if (f.t0 < a.V) {
             f.v = load_ids<DT>(in, f.t0, a.V, f.whole);
-            if (!f.whole) f.may = ids_of<N>(f.t0, a.V);
-            if (a.allowed != nullptr) f.may &= bits8(a.allowed + (static_cast<size_t>(b) * (a.P + 1) + f.ctx) * a.W, f.t0, 4 * a.W);
+            if (a.allowed != nullptr)
+                f.may = bits8(a.allowed + (static_cast<size_t>(b) * (a.P + 1) + context_row(a, b, side, r)) * a.W, f.t0, 4 * a.W);
         }
         return f;
     };
-    uint32_t used = 0u;
-    int used_at = INT_MIN;                                  // the id that `used` starts at
+    uint4 keep = make_uint4(0u, 0u, 0u, 0u);
+    int keep_at = INT_MIN;                                  // the id that `keep` starts at
     Row next = fetch(first);
     for (int q = first; q < last; ++q) {
         const Row f = next;
         if (q + 1 < last) next = fetch(q + 1);
         if (f.t0 >= a.V) continue;
-        if (history && f.t0 != used_at) { used = bits8(a.seen + static_cast<size_t>(b) * a.W, f.t0, 4 * a.W) & ((1u << N) - 1u); used_at = f.t0; }
-        const uint32_t sp = special.any ? bits8(special.bits, f.t0 - lo, sizeof(special.bits)) & ((1u << N) - 1u) : 0u;
-        const uint4 y = process_vec<DT>(a, p, b, f.ctx, f.t0, f.v, used, sp, f.may, [&](int t) { return counts[t - lo]; },
-                                        [&](int t) { return a.bias_offsets != nullptr ? special.bias[t - lo] : 0; });
+        uint4 y = process_vec<DT>(f.v, f.may, p.inv_temp);
+        if (n_sparse > 0) {
+            if (f.t0 != keep_at) { keep = spread_bits<DT>(bits8(sparse.bits, f.t0 - lo, sizeof(sparse.bits))); keep_at = f.t0; }
+            y = merge(y, f.v, keep);
+        }
         store_ids<DT>(f.out, f.t0, a.V, f.whole && f.alike, y);
+    }
+    if (n_sparse == 0) return;
+    __syncthreads();                                        // (what the block's threads stored is seen by all of them)
+    int k = threadIdx.x, q = first;
+    const auto turn = [&]() { while (k >= n_sparse && q < last) { k -= n_sparse; ++q; } return q < last; };
+    constexpr int kAtOnce = 4;
+    bool more = turn();
+    while (more) {
+        float x[kAtOnce];
+        elem* row[kAtOnce];
+        int id[kAtOnce], ctx[kAtOnce];
+        bool may[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            id[i] = -1;
+            if (!more) continue;
+            const int side = q >= a.rows[0], r = q - (side ? a.rows[0] : 0);
+            const size_t at = (static_cast<size_t>(b) * a.rows[side] + r) * a.V;
+            const int s = static_cast<int>(reinterpret_cast<uintptr_t>(static_cast<const elem*>(a.in[side]) + at) % 16 / sizeof(elem));
+            const int t = lo + sparse.list[k];
+            row[i] = static_cast<elem*>(a.out[side]) + at;
+            if (static_cast<unsigned>(t + s - span * kIds) < static_cast<unsigned>(kIds)) {       // (of the next block's, in this row)
+                id[i] = t;
+                ctx[i] = context_row(a, b, side, r);
+                x[i] = read_id<DT>(row[i], t);
+                may[i] = a.allowed == nullptr || (a.allowed[(static_cast<size_t>(b) * (a.P + 1) + ctx[i]) * a.W + (t >> 5)] >> (t & 31) & 1u);
+            }
+            k += kProcThreads;
+            more = turn();
+        }
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            if (id[i] < 0) continue;
+            const int at = id[i] - lo;
+            int d = 0, bias = 0;
+            if (sparse.drafted[at >> 5] >> (at & 31) & 1u) {
+                if (a.penalties) d = drafted(a, b, ctx[i], id[i]);
+                if (a.bias_offsets != nullptr) bias = sparse.bias[at];
+            }
+            const float y = process_id(x[i], sparse.counts[at], d, bias > 0 ? __ldg(a.bias_values + __ldg(a.bias_offsets + b) + bias - 1) : 0.f, bias > 0, p);
+            write_id<DT>(row[i], id[i], may[i] ? y : -INFINITY);
+        }
     }
 }
 

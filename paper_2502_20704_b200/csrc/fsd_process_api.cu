@@ -18,6 +18,7 @@ using namespace fsd;
 constexpr int kMaxV = 1 << 30;
 constexpr int kMaxNodes = 1024;        // as in the tree verification
 constexpr int kSMs = 148;
+constexpr size_t kCutSmem = 200 * 1024;    // dynamic shared memory of a block of the cut kernel at most; it has 13 KB of its own
 
 inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
@@ -42,11 +43,31 @@ int check(const fsd_process_opts* o) {
     return FSD_OK;
 }
 
+// How a row lies in the shared memory of a cluster's blocks.
+struct CutShape {
+    int blocks, slice;         // slice: vectors a block has
+    size_t smem;
+    bool fits;
+};
+template <int DT>
+CutShape cut_shape(const ProcArgs& a, bool raw) {
+    constexpr int N = Logit<DT>::kPerVec;
+    CutShape c;
+    const long long rows = static_cast<long long>(a.B) * (a.rows[0] + a.rows[1]);
+    const int vecs = (a.V + 2 * (N - 1)) / N;             // a row's, wherever it starts
+    c.blocks = 1;
+    while (c.blocks < kMaxCutCluster && (vecs > c.blocks * 4096ll || (rows * c.blocks < 2 * kSMs && vecs > c.blocks * 512ll))) c.blocks <<= 1;
+    c.slice = (vecs + c.blocks - 1) / c.blocks;
+    const bool drafts = !raw && a.penalties && a.tokens != nullptr;
+    c.smem = static_cast<size_t>(c.slice) * 16 + kBins * sizeof(uint32_t) + (drafts ? (static_cast<size_t>(c.slice) * N / 32 + 2) * sizeof(uint32_t) : 0);
+    c.fits = c.smem <= kCutSmem;
+    return c;
+}
+
 // Rows that are cut off: a cluster of blocks holds a row in shared memory where it fits, else a block sweeps over it in memory.
 template <int DT>
 int launch_cut(const ProcArgs& a, bool raw, cudaStream_t s) {
     constexpr int kDevices = 64;
-    constexpr size_t kMost = 200 * 1024;                  // of dynamic shared memory; the kernel has 7 KB of its own
     static bool ready[kDevices] = {};
     static std::mutex mu;
     int dev = 0;
@@ -54,45 +75,37 @@ int launch_cut(const ProcArgs& a, bool raw, cudaStream_t s) {
     {
         std::lock_guard<std::mutex> lock(mu);
         if (!ready[dev]) {
-            if (cudaFuncSetAttribute(fsd_cut_kernel<DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kMost)) != cudaSuccess) return FSD_ERR_CUDA;
+            if (cudaFuncSetAttribute(fsd_cut_kernel<DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kCutSmem)) != cudaSuccess) return FSD_ERR_CUDA;
             ready[dev] = true;
         }
     }
+    const CutShape c = cut_shape<DT>(a, raw);
     const long long rows = static_cast<long long>(a.B) * (a.rows[0] + a.rows[1]);
-    // a row's vectors, wherever it starts
-    const int vecs = (a.V + 2 * (Logit<DT>::kPerVec - 1)) / Logit<DT>::kPerVec;
-    const size_t bins = kBins * sizeof(uint32_t);
-    int blocks = 1;
-    while (blocks < kMaxCutCluster && (vecs > blocks * 4096 || (rows * blocks < 2 * kSMs && vecs > blocks * 512))) blocks <<= 1;
-    const int slice = (vecs + blocks - 1) / blocks;
-    const size_t smem = static_cast<size_t>(slice) * 16 + bins;
-    if (smem > kMost) {
-        if (rows > INT_MAX) return FSD_ERR_SHAPE;
+    if (rows * c.blocks > INT_MAX) return FSD_ERR_SHAPE;
+    if (!c.fits) {
         fsd_cut_long_kernel<DT><<<static_cast<unsigned>(rows), kLongThreads, 0, s>>>(a);
         return cudaGetLastError() == cudaSuccess ? FSD_OK : FSD_ERR_CUDA;
     }
-    if (rows * blocks > INT_MAX) return FSD_ERR_SHAPE;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(rows * blocks), 1, 1);
+    cfg.gridDim = dim3(static_cast<unsigned>(rows * c.blocks), 1, 1);
     cfg.blockDim = dim3(kRowThreads, 1, 1);
-    cfg.dynamicSmemBytes = smem;
+    cfg.dynamicSmemBytes = c.smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = static_cast<unsigned>(blocks); attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[0].val.clusterDim.x = static_cast<unsigned>(c.blocks); attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, fsd_cut_kernel<DT>, a, slice, raw) == cudaSuccess ? FSD_OK : FSD_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, fsd_cut_kernel<DT>, a, c.slice, raw) == cudaSuccess ? FSD_OK : FSD_ERR_CUDA;
 }
 
 template <int DT>
 int launch(const ProcArgs& a, bool cut, cudaStream_t s) {
     const int all = a.rows[0] + a.rows[1];
+    // The cut kernel does the rest too where the row stays on chip and there are no biases (whose lookup wants room there).
+    if (cut && a.bias_offsets == nullptr && cut_shape<DT>(a, false).fits) return launch_cut<DT>(a, false, s);
     // a row's vectors, wherever it starts, by blocks
     const long long spans = (a.V + 2 * (Logit<DT>::kPerVec - 1)) / Logit<DT>::kPerVec / kProcThreads + 1;
-    // The cut kernel does the rest too where the row stays on chip and there are no biases (whose lookup wants room there).
-    const bool together = cut && a.bias_offsets == nullptr && static_cast<long long>(a.V) * sizeof(typename Logit<DT>::elem) < kMaxCutCluster * 180000ll;
-    if (together) return launch_cut<DT>(a, false, s);
     // as many rows a block as leave eight blocks an SM, so that the counts are read for many rows at once
     long long group = spans * a.B * all / (8 * kSMs);
     group = group < 1 ? 1 : group > all ? all : group;

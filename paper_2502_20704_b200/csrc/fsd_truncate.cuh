@@ -257,8 +257,7 @@ struct CutShared {
     int found[4];
     double goal, above_goal;
     int warp_equal[kRowWarps + 1];
-    uint32_t special[256];     // a bit per 2^k vectors of the slice that hold a drafted token
-    int any_special;
+    uint16_t list[kRowWarps][256];
 };
 
 template <int DT> struct RowSlice {
@@ -643,18 +642,19 @@ __device__ __forceinline__ void words_of(const uint4& v, uint32_t (&bits)[Logit<
     }
 }
 
-// One value into the bins; those that share a bin with others of their size are weighed.
+// One value into the bins, or (BY -1) out of them; those that share a bin with others of their size are weighed.
+template <int BY>
 __device__ __noinline__ double count_value(uint32_t bits, uint32_t* hist) {
     if (bits == 0xff800000u) return 0.0;
     const uint32_t mag = bits >> 16 & 0x7fffu, u = (mag < kMagLo ? kMagLo : mag > kMagHi ? kMagHi : mag) - kMagLo;
     int bin = static_cast<int>(u ^ static_cast<uint32_t>(static_cast<int>(bits) >> 31)) + kHalfBins;
     if ((bits & 0x7fffffffu) > 0x7f800000u) bin = kBinOver;
-    atomicAdd(&hist[bin], 1u);
+    atomicAdd(&hist[bin], static_cast<uint32_t>(BY));
     return u != 0u ? 0.0 : (bits & 0x7fffffffu) == 0u ? 1.0 : exp(static_cast<double>(__uint_as_float(bits)));
 }
-// A vector of values into the bins; returns what is weighed.  bf16: two at a time, in halves of a word.
+// A vector of values, which `kept` has too, into the bins; returns what is weighed.  bf16: two at a time, in halves of a word.
 template <int DT>
-__device__ __forceinline__ double count_vec(const uint4& v, uint32_t* hist) {
+__device__ __forceinline__ double count_vec(const uint4& v, const uint4* kept, uint32_t* hist) {
     double tiny = 0.0;
     if constexpr (DT == FSD_BF16) {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -670,7 +670,7 @@ __device__ __forceinline__ double count_vec(const uint4& v, uint32_t* hist) {
         }
         if ((lowest & 0xffffu) == kMagLo || lowest >> 16 == kMagLo || (highest & 0xffffu) == kMagHi || highest >> 16 == kMagHi) {
 #pragma unroll 1
-            for (int e = 0; e < 8; ++e) tiny += count_value(__float_as_uint(id_of<DT>(v, e)), hist);
+            for (int e = 0; e < 8; ++e) tiny += count_value<1>(static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(kept)[e]) << 16, hist);
         } else {
             uint32_t* mid = hist + kHalfBins;
 #pragma unroll
@@ -684,7 +684,7 @@ __device__ __forceinline__ double count_vec(const uint4& v, uint32_t* hist) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const uint32_t mag = bits[e] >> 16 & 0x7fffu;
-            if (mag <= kMagLo || mag >= kMagHi) tiny += count_value(bits[e], hist);
+            if (mag <= kMagLo || mag >= kMagHi) tiny += count_value<1>(bits[e], hist);
             else atomicAdd(&hist[static_cast<int>((mag - kMagLo) ^ static_cast<uint32_t>(static_cast<int>(bits[e]) >> 31)) + kHalfBins], 1u);
         }
     }
@@ -699,6 +699,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_kernel(const ProcArgs 
     extern __shared__ uint4 on_chip[];
     __shared__ CutShared s;
     uint32_t* hist = reinterpret_cast<uint32_t*>(on_chip + slice);
+    uint32_t* drafted_ids = hist + kBins;                   // a bit for each of the slice's ids, from a multiple of 32 on; where tokens are drafted
     cg::cluster_group cluster = cg::this_cluster();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int blocks = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
@@ -717,25 +718,21 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_kernel(const ProcArgs 
     const SeqParams p = seq_params(a, b);
     const int ctx = context_row(a, b, side, r);
     const int drafts = !raw && a.penalties && a.tokens != nullptr ? a.P : 0;
-    int coarse = 0;                                         // 2^coarse vectors a bit
-    while ((slice >> coarse) > 256 * 32) ++coarse;
+    const int ids_lo = row.first > 0 ? row.first : 0, ids_hi = row.first + row.n * N < a.V ? row.first + row.n * N : a.V;   // of the slice
+    const int word0 = ids_lo >> 5, n_words = ids_hi > ids_lo ? (ids_hi + 31 >> 5) - word0 : 0;
     for (int i = tid; i < kBins; i += kRowThreads) hist[i] = 0u;
-    if (tid < 256) { s.special[tid] = 0u; s.sub_n[tid] = 0u; s.sub_w[tid] = 0u; }
-    if (tid == 0) s.any_special = 0;
+    if (drafts > 0)
+        for (int i = tid; i < n_words; i += kRowThreads) drafted_ids[i] = 0u;
+    if (tid < 256) { s.sub_n[tid] = 0u; s.sub_w[tid] = 0u; }
     __syncthreads();
     cluster_arrive();                                       // from here on others may add to the first block's counts
     for (int j = tid; j < drafts; j += kRowThreads) {
         const int t = __ldg(a.tokens + static_cast<size_t>(b) * a.P + j);
-        if (t >= 0 && t < a.V) {
-            const int v = (t + lies) / N - v0;
-            if (v >= 0 && v < row.n) {
-                atomicOr(&s.special[v >> coarse >> 5], 1u << (v >> coarse & 31));
-                s.any_special = 1;
-            }
-        }
+        if (t >= ids_lo && t < ids_hi) atomicOr(&drafted_ids[(t >> 5) - word0], 1u << (t & 31));
     }
-    __syncthreads();
-    const bool any_special = s.any_special != 0, history = a.penalties && a.seen != nullptr;
+    const bool history = !raw && a.penalties && a.seen != nullptr;
+    const uint32_t* seen = history ? a.seen + static_cast<size_t>(b) * a.W : nullptr;
+    const uint32_t* allowed = !raw && a.allowed != nullptr ? a.allowed + (static_cast<size_t>(b) * (a.P + 1) + ctx) * a.W : nullptr;
 
     // the slice: read, processed, counted, kept
     double tiny = 0.0;
@@ -746,25 +743,86 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_kernel(const ProcArgs 
         const bool whole = t0 >= 0 && t0 + N <= a.V;
         uint4 v = load_ids<DT>(in, t0, a.V, whole);
         if (!raw) {
-            uint32_t may = a.allowed != nullptr ? bits8(a.allowed + (static_cast<size_t>(b) * (a.P + 1) + ctx) * a.W, t0, 4 * a.W) : 0xffu;
+            uint32_t may = allowed != nullptr ? bits8(allowed, t0, 4 * a.W) : 0xffu;
             if (!whole) may &= ids_of<N>(t0, a.V);              // (what is not in the row counts as masked)
-            const uint32_t used = history ? bits8(a.seen + static_cast<size_t>(b) * a.W, t0, 4 * a.W) & ((1u << N) - 1u) : 0u;
-            const uint32_t sp = any_special && (s.special[i >> coarse >> 5] >> (i >> coarse & 31) & 1u) ? (1u << N) - 1u : 0u;
-            v = process_vec<DT>(a, p, b, ctx, t0, v, used, sp, may, [&](int t) { return __ldg(a.counts + static_cast<size_t>(b) * a.V + t); }, [](int) { return 0; });
-        }
-        if (!cutting) {
-            store_ids<DT>(out, t0, a.V, whole && alike, v);
-            continue;
-        }
-        tiny += count_vec<DT>(v, hist);
-        if constexpr (DT == FSD_F32) {
-            const uint32_t bits[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) { const uint32_t k = key_of<DT>(bits[e]); top = top > k ? top : k; }
+            v = process_vec<DT>(v, may, p.inv_temp);
         }
         row.vecs[i] = v;
+        if (!cutting) continue;
+        tiny += count_vec<DT>(v, row.vecs + i, hist);
+        if constexpr (DT == FSD_F32) {
+            const uint32_t bits[4] = {v.x, v.y, v.z, v.w};
+            const uint32_t sparse = (history ? bits8(seen, t0, 4 * a.W) : 0u) | (drafts > 0 ? bits8(drafted_ids, t0 - word0 * 32, 4 * n_words) : 0u);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t k = key_of<DT>(bits[e]);
+                if (!(sparse >> e & 1u)) top = top > k ? top : k;
+            }
+        }
     }
-    if (!cutting) { cluster_wait(); return; }               // (the whole cluster: it is the sequence that asks)
+    // Then the ids that are used or drafted, one a thread: what was counted for them without a penalty is taken back.  A warp takes
+    // 32 words of the bitmaps at a time and lists their bits, so that its threads have as many each.
+    if (history || drafts > 0) {
+        __syncthreads();
+        LogitWord<DT>* words = reinterpret_cast<LogitWord<DT>*>(row.vecs) - row.first;      // by id
+        for (int w0 = warp * 32; w0 < n_words; w0 += kRowWarps * 32) {
+            const int w = w0 + lane;
+            uint32_t used = 0u, draft = 0u;
+            if (w < n_words) {
+                uint32_t may = allowed != nullptr ? allowed[word0 + w] : 0xffffffffu;
+                const int t = (word0 + w) * 32;
+                if (t < ids_lo) may &= 0xffffffffu << (ids_lo - t);
+                if (t + 32 > ids_hi) may &= 0xffffffffu >> (t + 32 - ids_hi);
+                used = history ? __ldg(seen + word0 + w) & may : 0u;
+                draft = drafts > 0 ? drafted_ids[w] & may : 0u;
+            }
+            uint32_t todo = used | draft;
+            int at = __popc(todo);
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int o = __shfl_up_sync(0xffffffffu, at, d);
+                if (lane >= d) at += o;
+            }
+            const int total = __shfl_sync(0xffffffffu, at, 31);
+            at -= __popc(todo);
+            for (int base = 0; base < total; base += 256) {
+                while (todo != 0u && at < base + 256) {
+                    s.list[warp][at - base] = static_cast<uint16_t>(lane * 32 + __ffs(static_cast<int>(todo)) - 1);
+                    todo &= todo - 1u;
+                    ++at;
+                }
+                __syncwarp();
+                const int n = total - base < 256 ? total - base : 256;
+#pragma unroll 2
+                for (int k0 = 0; k0 < n; k0 += 32) {
+                    const int k = k0 + lane, l = k < n ? s.list[warp][k] : 0;
+                    const uint32_t is_used = __shfl_sync(0xffffffffu, used, l >> 5) >> (l & 31) & 1u;
+                    const uint32_t is_draft = __shfl_sync(0xffffffffu, draft, l >> 5) >> (l & 31) & 1u;
+                    if (k >= n) continue;
+                    const int t = (word0 + w0) * 32 + l;
+                    const int count = is_used ? __ldg(a.counts + static_cast<size_t>(b) * a.V + t) : -1;
+                    const float x = read_id<DT>(in, t);
+                    const int d = is_draft ? drafted(a, b, ctx, t) : 0;
+                    const uint32_t before = words[t];
+                    write_id<DT>(words, t, process_id(x, count, d, 0.f, false, p));
+                    if (!cutting) continue;
+                    const uint32_t now = words[t];
+                    tiny += count_value<1>(__float_as_uint(float_of<DT>(now)), hist) - count_value<-1>(__float_as_uint(float_of<DT>(before)), hist);
+                    if constexpr (DT == FSD_F32) { const uint32_t key = key_of<DT>(now); top = top > key ? top : key; }
+                }
+                __syncwarp();
+            }
+        }
+    }
+    if (!cutting) {                                         // (the whole cluster: it is the sequence that asks)
+        __syncthreads();
+        for (int i = tid; i < row.n; i += kRowThreads) {
+            const int t0 = row.first + i * N;
+            store_ids<DT>(out, t0, a.V, t0 >= 0 && t0 + N <= a.V && alike, row.vecs[i]);
+        }
+        cluster_wait();
+        return;
+    }
 
     CutShared& first = *cluster.map_shared_rank(&s, 0);
     const CountAndWeight tiny_all = block_total({0, tiny}, s.scratch);
