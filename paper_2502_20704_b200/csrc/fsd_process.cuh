@@ -261,86 +261,75 @@ __global__ void __launch_bounds__(kProcThreads) fsd_process_kernel(const ProcArg
     const SeqParams p = seq_params(a, b);
     const int all = a.rows[0] + a.rows[1], first = group * group_rows, last = first + group_rows < all ? first + group_rows : all;
 
-    struct Row {                                            // a row's vector on the way
-        uint4 v;
-        uint32_t may;
-        int t0;
-        elem* out;
-        bool whole, alike;
-    };
-    const auto fetch = [&](int q) {
-        Row f;
-        const int side = q >= a.rows[0], r = q - (side ? a.rows[0] : 0);
-        const size_t at = (static_cast<size_t>(b) * a.rows[side] + r) * a.V;
-        const elem* in = static_cast<const elem*>(a.in[side]) + at;
-        f.out = static_cast<elem*>(a.out[side]) + at;
-        const int s = static_cast<int>(reinterpret_cast<uintptr_t>(in) % 16 / sizeof(elem));
-        f.alike = (reinterpret_cast<uintptr_t>(in) ^ reinterpret_cast<uintptr_t>(f.out)) % 16 == 0;
-        f.t0 = (span * kProcThreads + static_cast<int>(threadIdx.x)) * N - s;
-        f.whole = f.t0 >= 0 && f.t0 + N <= a.V;
-        f.may = 0xffu;
-        f.v = make_uint4(0u, 0u, 0u, 0u);
-        if (f.t0 < a.V) {
-            f.v = load_ids<DT>(in, f.t0, a.V, f.whole);
-            if (a.allowed != nullptr)
-                f.may = bits8(a.allowed + (static_cast<size_t>(b) * (a.P + 1) + context_row(a, b, side, r)) * a.W, f.t0, 4 * a.W);
-        }
-        return f;
-    };
+    const uint32_t* allowed = a.allowed != nullptr ? a.allowed + static_cast<size_t>(b) * (a.P + 1) * a.W : nullptr;
     uint4 keep = make_uint4(0u, 0u, 0u, 0u);
     int keep_at = INT_MIN;                                  // the id that `keep` starts at
-    Row next = fetch(first);
-    for (int q = first; q < last; ++q) {
-        const Row f = next;
-        if (q + 1 < last) next = fetch(q + 1);
-        if (f.t0 >= a.V) continue;
-        uint4 y = process_vec<DT>(f.v, f.may, p.inv_temp);
-        if (n_sparse > 0) {
-            if (f.t0 != keep_at) { keep = spread_bits<DT>(bits8(sparse.bits, f.t0 - lo, sizeof(sparse.bits))); keep_at = f.t0; }
-            y = merge(y, f.v, keep);
+#pragma unroll 1
+    for (int side = 0; side < 2; ++side) {
+        const int r0 = side == 0 ? first : (first > a.rows[0] ? first - a.rows[0] : 0);
+        const int r1 = side == 0 ? (last < a.rows[0] ? last : a.rows[0]) : last - a.rows[0];
+        if (r0 >= r1) continue;
+        const size_t at = (static_cast<size_t>(b) * a.rows[side] + r0) * a.V;
+        const elem* in = static_cast<const elem*>(a.in[side]) + at;
+        elem* out = static_cast<elem*>(a.out[side]) + at;
+        const bool alike = (reinterpret_cast<uintptr_t>(in) ^ reinterpret_cast<uintptr_t>(out)) % 16 == 0;
+        const int base = (span * kProcThreads + static_cast<int>(threadIdx.x)) * N;
+        struct Row {                                        // a row's vector on the way
+            uint4 v;
+            uint32_t may;
+        };
+        const auto first_id = [&](const elem* row) { return base - static_cast<int>(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(elem)); };
+        const auto fetch = [&](const elem* row, int r) {
+            Row f = {make_uint4(0u, 0u, 0u, 0u), 0xffu};
+            const int t0 = first_id(row);
+            if (t0 < a.V) {
+                if (allowed != nullptr) f.may = bits8(allowed + static_cast<size_t>(context_row(a, b, side, r)) * a.W, t0, 4 * a.W);
+                f.v = load_ids<DT>(row, t0, a.V, t0 >= 0 && t0 + N <= a.V);
+            }
+            return f;
+        };
+        Row next = fetch(in, r0);
+#pragma unroll 2
+        for (int r = r0; r < r1; ++r) {
+            const Row f = next;
+            const int t0 = first_id(in);
+            in += a.V;
+            if (r + 1 < r1) next = fetch(in, r + 1);
+            if (t0 < a.V) {
+                uint4 y = process_vec<DT>(f.v, f.may, p.inv_temp);
+                if (n_sparse > 0) {
+                    if (t0 != keep_at) { keep = spread_bits<DT>(bits8(sparse.bits, t0 - lo, sizeof(sparse.bits))); keep_at = t0; }
+                    y = merge(y, f.v, keep);
+                }
+                store_ids<DT>(out, t0, a.V, t0 >= 0 && t0 + N <= a.V && alike, y);
+            }
+            out += a.V;
         }
-        store_ids<DT>(f.out, f.t0, a.V, f.whole && f.alike, y);
     }
     if (n_sparse == 0) return;
     __syncthreads();                                        // (what the block's threads stored is seen by all of them)
-    int k = threadIdx.x, q = first;
-    const auto turn = [&]() { while (k >= n_sparse && q < last) { k -= n_sparse; ++q; } return q < last; };
-    constexpr int kAtOnce = 4;
-    bool more = turn();
-    while (more) {
-        float x[kAtOnce];
-        elem* row[kAtOnce];
-        int id[kAtOnce], ctx[kAtOnce];
-        bool may[kAtOnce];
-#pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            id[i] = -1;
-            if (!more) continue;
+    // `wide` threads a row, each with the same id in all rows it does
+    int wide = 32;
+    while (wide < kProcThreads && wide < n_sparse) wide <<= 1;
+    const int stride = kProcThreads / wide;
+    for (int k = static_cast<int>(threadIdx.x) % wide; k < n_sparse; k += wide) {
+        const int at = sparse.list[k], t = lo + at, count = sparse.counts[at];
+        const bool again = sparse.drafted[at >> 5] >> (at & 31) & 1u;
+        const int entry = again && a.bias_offsets != nullptr ? sparse.bias[at] : 0;
+        const float bias = entry > 0 ? __ldg(a.bias_values + __ldg(a.bias_offsets + b) + entry - 1) : 0.f;
+#pragma unroll 4
+        for (int q = first + static_cast<int>(threadIdx.x) / wide; q < last; q += stride) {
             const int side = q >= a.rows[0], r = q - (side ? a.rows[0] : 0);
-            const size_t at = (static_cast<size_t>(b) * a.rows[side] + r) * a.V;
-            const int s = static_cast<int>(reinterpret_cast<uintptr_t>(static_cast<const elem*>(a.in[side]) + at) % 16 / sizeof(elem));
-            const int t = lo + sparse.list[k];
-            row[i] = static_cast<elem*>(a.out[side]) + at;
-            if (static_cast<unsigned>(t + s - span * kIds) < static_cast<unsigned>(kIds)) {       // (of the next block's, in this row)
-                id[i] = t;
-                ctx[i] = context_row(a, b, side, r);
-                x[i] = read_id<DT>(row[i], t);
-                may[i] = a.allowed == nullptr || (a.allowed[(static_cast<size_t>(b) * (a.P + 1) + ctx[i]) * a.W + (t >> 5)] >> (t & 31) & 1u);
-            }
-            k += kProcThreads;
-            more = turn();
-        }
-#pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            if (id[i] < 0) continue;
-            const int at = id[i] - lo;
-            int d = 0, bias = 0;
-            if (sparse.drafted[at >> 5] >> (at & 31) & 1u) {
-                if (a.penalties) d = drafted(a, b, ctx[i], id[i]);
-                if (a.bias_offsets != nullptr) bias = sparse.bias[at];
-            }
-            const float y = process_id(x[i], sparse.counts[at], d, bias > 0 ? __ldg(a.bias_values + __ldg(a.bias_offsets + b) + bias - 1) : 0.f, bias > 0, p);
-            write_id<DT>(row[i], id[i], may[i] ? y : -INFINITY);
+            const size_t line = (static_cast<size_t>(b) * a.rows[side] + r) * a.V;
+            const int s = static_cast<int>(reinterpret_cast<uintptr_t>(static_cast<const elem*>(a.in[side]) + line) % 16 / sizeof(elem));
+            if (static_cast<unsigned>(t + s - span * kIds) >= static_cast<unsigned>(kIds)) continue;      // (another block's, in this row)
+            elem* row = static_cast<elem*>(a.out[side]) + line;
+            int ctx = 0, d = 0;
+            if (again || allowed != nullptr) ctx = context_row(a, b, side, r);
+            if (again && a.penalties) d = drafted(a, b, ctx, t);
+            const bool may = allowed == nullptr || (__ldg(allowed + static_cast<size_t>(ctx) * a.W + (t >> 5)) >> (t & 31) & 1u);
+            const float y = process_id(read_id<DT>(row, t), count, d, bias, entry > 0, p);
+            write_id<DT>(row, t, may ? y : -INFINITY);
         }
     }
 }

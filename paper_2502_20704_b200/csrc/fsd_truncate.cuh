@@ -691,6 +691,58 @@ __device__ __forceinline__ double count_vec(const uint4& v, const uint4* kept, u
     return tiny;
 }
 
+// How many of a vector's values are equal to one.
+template <int DT>
+__device__ __forceinline__ int equal_in(const uint4& v, float value) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t n = 0u;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if constexpr (DT == FSD_BF16)
+            n += __heq2_mask(*reinterpret_cast<const __nv_bfloat162*>(&w[k]), __bfloat162bfloat162(__float2bfloat16_rn(value))) & 0x10001u;
+        else n += __uint_as_float(w[k]) == value;
+    }
+    return static_cast<int>(DT == FSD_BF16 ? (n & 0xffffu) + (n >> 16) : n);
+}
+// A vector with -inf for what is below the cut, and (above) for what is equal to it.
+template <int DT>
+__device__ __forceinline__ uint4 cut_vec(const uint4& v, float value, bool above) {
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    if constexpr (DT == FSD_BF16) {
+        const __nv_bfloat162 cut = __bfloat162bfloat162(__float2bfloat16_rn(value));      // (it is a value of bf16)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const __nv_bfloat162 y = *reinterpret_cast<const __nv_bfloat162*>(&w[k]);
+            const uint32_t keep = above ? __hgt2_mask(y, cut) : __hge2_mask(y, cut);
+            w[k] = (w[k] & keep) | (0xff80ff80u & ~keep);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float y = __uint_as_float(w[k]);
+            w[k] = (above ? y > value : y >= value) ? w[k] : 0xff800000u;
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// A vector of which at most `left` of those equal to the cut are kept, and none from its id number `end` on.
+template <int DT>
+__device__ __noinline__ uint4 cut_some(uint4 v, float value, int left, int end) {
+    constexpr int N = Logit<DT>::kPerVec;
+    uint32_t bits[N];
+    words_of<DT>(v, bits);
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        const float y = __uint_as_float(bits[e]);
+        const bool at = y == value, keep = y > value || (at && left > 0 && e < end);
+        left -= at;
+        if (!keep) bits[e] = 0xff800000u;
+    }
+    if constexpr (DT == FSD_BF16)
+        return make_uint4(bits[0] >> 16 | bits[1], bits[2] >> 16 | bits[3], bits[4] >> 16 | bits[5], bits[6] >> 16 | bits[7]);
+    else return make_uint4(bits[0], bits[1], bits[2], bits[3]);
+}
+
 // raw: the rows are processed already.
 template <int DT>
 __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_kernel(const ProcArgs a, int slice, bool raw) {
@@ -878,17 +930,11 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_kernel(const ProcArgs 
     }
     const long long ties = res.kind == kCutDone ? res.ties : a.V;
     const float value = value_of<DT>(key);
-    // where only the first `ties` of the tokens at the cut are kept, each warp has a run of the slice and counts those before it
+    // Where only the first `ties` of the tokens at the cut are kept, each warp has a run of the slice and counts those before it.
     const int run = (row.n + kRowWarps - 1) / kRowWarps, w0 = warp * run < row.n ? warp * run : row.n, w1 = w0 + run < row.n ? w0 + run : row.n;
-    long long before = 0;
+    int left = INT_MAX, mine = 0;                           // how many of those in the warp's run are kept, and how many there are
     if (ties < a.V) {
-        int mine = 0;
-        for (int i = w0 + lane; i < w1; i += 32) {
-            uint32_t bits[N];
-            words_of<DT>(row.vecs[i], bits);
-#pragma unroll
-            for (int e = 0; e < N; ++e) mine += __uint_as_float(bits[e]) == value;
-        }
+        for (int i = w0 + lane; i < w1; i += 32) mine += equal_in<DT>(row.vecs[i], value);
         mine = __reduce_add_sync(0xffffffffu, mine);
         if (lane == 0) s.warp_equal[warp] = mine;
         __syncthreads();
@@ -896,72 +942,37 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_kernel(const ProcArgs 
         for (int w = 0; w < kRowWarps; ++w) { if (w == warp) ahead = sum; sum += s.warp_equal[w]; }
         if (tid < blocks) cluster.map_shared_rank(&s, tid)->equal[rank] = sum;
         cluster_barrier();
+        long long before = ahead;
         for (int k = 0; k < rank; ++k) before += s.equal[k];
-        before += ahead;
+        left = ties <= before ? 0 : ties - before < mine ? static_cast<int>(ties - before) : INT_MAX;
     }
-    if (ties >= a.V && until >= a.V) {                      // all that are equal to the cut are kept
-        for (int i = tid; i < row.n; i += kRowThreads) {
-            uint4 v = row.vecs[i];
-            if (!keep_all) {
-                if constexpr (DT == FSD_BF16) {
-                    uint32_t w[4] = {v.x, v.y, v.z, v.w};
-                    const __nv_bfloat162 cut2 = __bfloat162bfloat162(__float2bfloat16_rn(value));       // (value is one of bf16)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const uint32_t keep = __hge2_mask(*reinterpret_cast<const __nv_bfloat162*>(&w[k]), cut2);
-                        w[k] = (w[k] & keep) | (0xff80ff80u & ~keep);
-                    }
-                    v = make_uint4(w[0], w[1], w[2], w[3]);
-                } else {
-                    v.x = __uint_as_float(v.x) >= value ? v.x : 0xff800000u;
-                    v.y = __uint_as_float(v.y) >= value ? v.y : 0xff800000u;
-                    v.z = __uint_as_float(v.z) >= value ? v.z : 0xff800000u;
-                    v.w = __uint_as_float(v.w) >= value ? v.w : 0xff800000u;
-                }
-            }
-            const int t0 = row.first + i * N;
-            store_ids<DT>(out, t0, a.V, t0 >= 0 && t0 + N <= a.V && alike, v);
-        }
-        return;
-    }
+    const bool some = left > 0 && left != INT_MAX;          // the one run that the last of them is in
+    const bool above = left == 0;                           // none in this run: what is kept is above the cut
     for (int i0 = w0; i0 < w1; i0 += 32) {
         const int i = i0 + lane;
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        uint32_t bits[N];
-        int equal = 0;
-        if (i < w1) v = row.vecs[i];
-        words_of<DT>(v, bits);
-        long long ahead = before;
-        if (ties < a.V) {
-            if (i < w1) {
-#pragma unroll
-                for (int e = 0; e < N; ++e) equal += __uint_as_float(bits[e]) == value;
-            }
-            int sum = equal;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int o = __shfl_up_sync(0xffffffffu, sum, d);
-                if (lane >= d) sum += o;
-            }
-            ahead = before + sum - equal;
-            before += __shfl_sync(0xffffffffu, sum, 31);
-        }
-        if (i >= w1) continue;
+        const bool in_run = i < w1;
+        uint4 v = in_run ? row.vecs[i] : make_uint4(0u, 0u, 0u, 0u);
         const int t0 = row.first + i * N;
-        {
-            uint32_t out_bits[N];
+        if (some || until < a.V) {
+            if (some) {
+                const int equal = in_run ? equal_in<DT>(v, value) : 0;
+                int sum = equal;
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const float y = __uint_as_float(bits[e]);
-                bool keep = y > value || (y == value && t0 + e < until);
-                if (ties < a.V && y == value) { keep = ahead < ties; ++ahead; }
-                out_bits[e] = keep ? bits[e] : 0xff800000u;
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int o = __shfl_up_sync(0xffffffffu, sum, d);
+                    if (lane >= d) sum += o;
+                }
+                const int rank_of = sum - equal;            // of the run's tokens at the cut, how many are before this vector's
+                const int all_of_them = __shfl_sync(0xffffffffu, sum, 31);
+                v = cut_some<DT>(v, value, left - rank_of, N);
+                left -= all_of_them;
+            } else {
+                v = cut_some<DT>(v, value, INT_MAX, until - t0);
             }
-            if constexpr (DT == FSD_BF16)
-                v = make_uint4(out_bits[0] >> 16 | out_bits[1], out_bits[2] >> 16 | out_bits[3], out_bits[4] >> 16 | out_bits[5], out_bits[6] >> 16 | out_bits[7]);
-            else v = make_uint4(out_bits[0], out_bits[1], out_bits[2], out_bits[3]);
+        } else if (!keep_all) {
+            v = cut_vec<DT>(v, value, above);
         }
-        store_ids<DT>(out, t0, a.V, t0 >= 0 && t0 + N <= a.V && alike, v);
+        if (in_run) store_ids<DT>(out, t0, a.V, t0 >= 0 && t0 + N <= a.V && alike, v);
     }
 }
 
