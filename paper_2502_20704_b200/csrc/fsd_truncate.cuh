@@ -41,12 +41,12 @@ struct CutParams {
     float top_p, min_p;
     bool k, p, m;
 };
-__device__ __forceinline__ CutParams cut_params(const ProcArgs& a, int b) {
+__device__ __forceinline__ CutParams cut_params(const uint32_t* settings, int V) {      // top_k, top_p, min_p
     CutParams c;
-    c.top_k = a.top_k != nullptr ? __ldg(a.top_k + b) : 0;
-    c.top_p = a.top_p != nullptr ? __ldg(a.top_p + b) : 1.f;
-    c.min_p = a.min_p != nullptr ? __ldg(a.min_p + b) : 0.f;
-    c.k = c.top_k > 0 && c.top_k < a.V;
+    c.top_k = static_cast<int>(settings[0]);
+    c.top_p = __uint_as_float(settings[1]);
+    c.min_p = __uint_as_float(settings[2]);
+    c.k = c.top_k > 0 && c.top_k < V;
     c.p = c.top_p < 1.f;
     c.m = c.min_p > 0.f;
     return c;
@@ -63,26 +63,48 @@ __device__ __forceinline__ long long ties_below(double above, double w, double g
 // (Out of line: the places that need it are many and reached seldom.)
 __device__ __noinline__ double exp_d(double x) { return exp(x); }
 
-// The smallest key whose value is no further below the largest, `most` with key `top`, than ln(min_p).  A whole warp.
+// exp(x) for x of at most 700, to a few units of the last place: x = n ln 2 + r with |r| <= ln 2 / 2, and e^r by its
+// Taylor series up to r^13 / 13! (the next term is below 5e-18).  Sums that say where a border lies need that much of each of
+// their terms.  Below -700 it is 0.
+__device__ __forceinline__ double exp_of(double x) {
+    if (!(x > -700.0)) return 0.0;
+    const double shift = 6755399441055744.0;                                      // 1.5 * 2^52: adding it rounds to a whole number
+    const double u = __fma_rn(x, kLog2eD, shift);
+    const int n = __double2loint(u);
+    const double m = u - shift;
+    const double r = __fma_rn(m, -2.3190468138462996e-17, __fma_rn(m, -0.69314718055994529, x));      // ln 2 as a double and what it lacks
+    double e = 1.0 / 6227020800.0;
+    e = __fma_rn(e, r, 1.0 / 479001600.0);
+    e = __fma_rn(e, r, 1.0 / 39916800.0);
+    e = __fma_rn(e, r, 1.0 / 3628800.0);
+    e = __fma_rn(e, r, 1.0 / 362880.0);
+    e = __fma_rn(e, r, 1.0 / 40320.0);
+    e = __fma_rn(e, r, 1.0 / 5040.0);
+    e = __fma_rn(e, r, 1.0 / 720.0);
+    e = __fma_rn(e, r, 1.0 / 120.0);
+    e = __fma_rn(e, r, 1.0 / 24.0);
+    e = __fma_rn(e, r, 1.0 / 6.0);
+    e = __fma_rn(e, r, 0.5);
+    e = __fma_rn(e, r, 1.0);
+    e = __fma_rn(e, r, 1.0);
+    return __hiloint2double(__double2hiint(e) + (n << 20), __double2loint(e));     // (|n| is at most 1010: no subnormals)
+}
+
+// The smallest key whose value is no further below the largest, `most` with key `top`, than ln(min_p).  It is at the value
+// most + ln(min_p) or next to it, unless the difference to `most` does not tell values there apart.
 template <int DT>
 __device__ __noinline__ uint32_t min_p_key(float min_p, uint32_t top, double most) {
     const double far = log(static_cast<double>(min_p < 1.f ? min_p : 1.f));
-    const uint32_t lane = threadIdx.x & 31;
+    const auto in = [&](uint32_t k) { return static_cast<double>(value_of<DT>(k)) - most >= far; };
     uint32_t lo = key_of_value<DT>(-INFINITY), hi = top;        // hi always is, lo never
+    const uint32_t guess = key_of_value<DT>(static_cast<float>(most + far));
+    if (guess > lo + 2u && guess + 2u < hi) {
+        if (in(guess + 2u)) hi = guess + 2u;
+        if (!in(guess - 2u)) lo = guess - 2u;
+    }
     while (hi - lo > 1u) {
-        const uint32_t step = (hi - lo) / 33u + 1u;
-        const auto at = [&](uint32_t k) { return step * k < hi - lo ? lo + step * k : hi; };
-        const uint32_t is = __ballot_sync(0xffffffffu, static_cast<double>(value_of<DT>(at(lane + 1u))) - most >= far) | 1u << 31;
-        const uint32_t k = __ffs(static_cast<int>(is)) - 1;     // (where no lane below the last is, the last may not be either: hi stays)
-        const bool last = __shfl_sync(0xffffffffu, static_cast<double>(value_of<DT>(at(32u))) - most >= far, 0);
-        const uint32_t old_lo = lo, old_hi = hi;
-        const auto from = [&](uint32_t j) { return step * j < old_hi - old_lo ? old_lo + step * j : old_hi; };
-        if (k == 31u && !last) {
-            lo = from(32u);
-        } else {
-            lo = k == 0u ? old_lo : from(k);
-            hi = from(k + 1u);
-        }
+        const uint32_t mid = lo + (hi - lo) / 2u;
+        if (in(mid)) hi = mid; else lo = mid;
     }
     return hi;
 }
@@ -197,7 +219,9 @@ __global__ void __launch_bounds__(kLongThreads) fsd_cut_long_kernel(const ProcAr
     const int all = a.rows[0] + a.rows[1], b = blockIdx.x / all, q = blockIdx.x % all;
     const int side = q >= a.rows[0], r = q - (side ? a.rows[0] : 0);
     LogitWord<DT>* row = static_cast<LogitWord<DT>*>(a.out[side]) + (static_cast<size_t>(b) * a.rows[side] + r) * a.V;
-    const CutParams c = cut_params(a, b);
+    const uint32_t settings[3] = {a.top_k != nullptr ? static_cast<uint32_t>(__ldg(a.top_k + b)) : 0u, __float_as_uint(a.top_p != nullptr ? __ldg(a.top_p + b) : 1.f),
+                                  __float_as_uint(a.min_p != nullptr ? __ldg(a.min_p + b) : 0.f)};
+    const CutParams c = cut_params(settings, a.V);
     if (!c.k && !c.p && !c.m) return;
     const Cut cut = find_cut<DT>(row, a.V, 0, a.V, c, [&](CountAndWeight v) { return block_total(v, scratch); }, [&](uint32_t k) { return block_largest(k, scratch); });
     if (!cut.any) return;
@@ -250,6 +274,10 @@ struct CutShared {
     int equal[kMaxCutCluster];
     CountAndWeight slots[2][kMaxCutCluster];
     CountAndWeight scratch[32];
+    uint32_t warp_n[kRowWarps];
+    double warp_w[kRowWarps];
+    uint32_t min_key;
+    uint32_t settings[8];
     uint64_t sub_w[256];
     uint32_t sub_n[256];
     CutResult work;            // the first block's
@@ -271,161 +299,177 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 __device__ __forceinline__ void cluster_barrier() { cluster_arrive(); cluster_wait(); }
 
 // Exclusive sums over the threads of the block, in thread order.  All threads; ends with a barrier.
-__device__ __forceinline__ CountAndWeight scan_threads(CountAndWeight v, CountAndWeight* scratch, CountAndWeight& all) {
+struct Run {
+    uint32_t n;
+    double w;
+};
+__device__ __forceinline__ Run scan_threads(Run v, CutShared& s, Run& all) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    CountAndWeight s = v;
+    Run t = v;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const long long n = __shfl_up_sync(0xffffffffu, s.n, d);
-        const double w = __shfl_up_sync(0xffffffffu, s.w, d);
-        if (lane >= d) { s.n += n; s.w += w; }
+        const uint32_t n = __shfl_up_sync(0xffffffffu, t.n, d);
+        const double w = __shfl_up_sync(0xffffffffu, t.w, d);
+        if (lane >= d) { t.n += n; t.w += w; }
     }
-    if (lane == 31) scratch[warp] = s;
-    CountAndWeight e;
-    e.n = __shfl_up_sync(0xffffffffu, s.n, 1);
-    e.w = __shfl_up_sync(0xffffffffu, s.w, 1);
-    if (lane == 0) e = {0, 0.0};
+    if (lane == 31) { s.warp_n[warp] = t.n; s.warp_w[warp] = t.w; }
+    Run e;
+    e.n = __shfl_up_sync(0xffffffffu, t.n, 1);
+    e.w = __shfl_up_sync(0xffffffffu, t.w, 1);
+    if (lane == 0) e = {0u, 0.0};
     __syncthreads();
-    all = {0, 0.0};
-    const int warps = blockDim.x >> 5;
-    for (int w = 0; w < warps; ++w) {
-        if (w == warp) { e.n += all.n; e.w += all.w; }
-        all.n += scratch[w].n; all.w += scratch[w].w;
+    all = {0u, 0.0};
+    Run ahead = {0u, 0.0};
+#pragma unroll
+    for (int w = 0; w < kRowWarps; ++w) {
+        if (w == warp) ahead = all;
+        all.n += s.warp_n[w];
+        all.w += s.warp_w[w];
     }
+    e.n += ahead.n;
+    e.w += ahead.w;
     __syncthreads();
     return e;
 }
 
-// The first block: from the counts of all to the cut (bf16) or to the bins that hold the cuts (fp32).
+// The first block: from the counts of all to the cut (bf16) or to the bins that hold the cuts (fp32).  `place` counts bins from
+// the highest one down, a thread has kBinsEach of them.
 template <int DT>
-__device__ void solve_bins(const uint32_t* hist, CutShared& s, const CutParams& c, int blocks, int V) {
+__device__ __forceinline__ void solve_bins(const uint32_t* hist, CutShared& s, const CutParams& c, int blocks, int V) {
     const int tid = threadIdx.x;
-    if (tid < 4) s.found[tid] = tid == 0 ? -1 : kBins;       // 0: bin of the k-th, 1: place of the highest bin, 2: place of the border of top-p
+    if (tid == 0) {
+        s.found[0] = -1;                                     // place of the k-th token
+        s.found[1] = s.found[2] = kBins;                     // of the highest one, and of the border of top-p
+        s.work = {kCutDone, 0u, V, 0u};
+        s.min_key = 0u;
+    }
     uint32_t n[kBinsEach];
-    CountAndWeight mine = {0, 0.0};
     double w[kBinsEach];
-    double tiny = 0.0;
-    for (int k = 0; k < blocks; ++k) tiny += s.tiny[k];
+    Run mine = {0u, 0.0};
+    static_assert(kBinsEach % 4 == 0 && kBins % 4 == 0, "whole vectors of bins");
 #pragma unroll
-    for (int j = 0; j < kBinsEach; ++j) {
-        const int bin = kBins - 1 - (tid * kBinsEach + j);
-        n[j] = bin >= 0 ? hist[bin] : 0u;
-        w[j] = 0.0;
-        if (n[j] != 0u && one_value(bin)) w[j] = exp_d(bin_value<DT>(bin));
-        mine.n += n[j];
-        mine.w += bin == kBinTinyPos ? tiny : n[j] * w[j];
+    for (int j = 0; j < kBinsEach; j += 4) {
+        const int bin = kBins - 4 - (tid * kBinsEach + j);
+        const uint4 v = bin >= 0 ? *reinterpret_cast<const uint4*>(hist + bin) : make_uint4(0u, 0u, 0u, 0u);
+        n[j] = v.w; n[j + 1] = v.z; n[j + 2] = v.y; n[j + 3] = v.x;
+        mine.n += v.x + v.y + v.z + v.w;
     }
-    if (tid == 0) s.work = {kCutDone, 0u, V, 0u};
-    CountAndWeight all;
-    const CountAndWeight before = scan_threads(mine, s.scratch, all);
-    const bool cut_k = c.k && all.n > c.top_k;
-    // the highest bin, and that of the k-th token
-    CountAndWeight run = before;
+    double tiny = 0.0;                                       // the thread of that bin has what those weigh that share it
+    if (tid == (kBins - 1 - kBinTinyPos) / kBinsEach) {
 #pragma unroll
-    for (int j = 0; j < kBinsEach; ++j) {
-        const int place = tid * kBinsEach + j, bin = kBins - 1 - place;
-        if (n[j] != 0u) {
-            if (run.n == 0) s.found[1] = place;
-            if (cut_k && run.n < c.top_k && run.n + n[j] >= c.top_k) {
-                s.found[0] = place;
-                s.work.ties = c.top_k - run.n;
-                s.above_goal = run.w;                       // what stands above this bin weighs
-                if (one_value(bin)) s.goal = run.w + static_cast<double>(c.top_k - run.n) * w[j];
-            }
+        for (int k = 0; k < kMaxCutCluster; ++k) tiny += k < blocks ? s.tiny[k] : 0.0;
+    }
+#pragma unroll
+    for (int j = 0; j < kBinsEach; ++j) w[j] = 0.0;
+    if (mine.n != 0u) {
+#pragma unroll
+        for (int j = 0; j < kBinsEach; ++j) {
+            const int bin = kBins - 1 - (tid * kBinsEach + j);
+            w[j] = one_value(bin) ? exp_of(bin_value<DT>(bin)) : 0.0;
+            mine.w += n[j] * w[j];
         }
-        run.n += n[j];
-        run.w += bin == kBinTinyPos ? tiny : n[j] * w[j];
     }
-    __syncthreads();
-    const int top_bin = kBins - 1 - s.found[1], k_place = s.found[0], k_bin = kBins - 1 - k_place;
-    if (all.n == 0) {                                       // nothing finite, and nothing above it either
+    mine.w += tiny;
+    Run all;
+    const Run before = scan_threads(mine, s, all);
+    const bool cut_k = c.k && all.n > static_cast<uint32_t>(c.top_k);
+    if (all.n == 0u) {                                       // nothing finite, and nothing above it either
         if (tid == 0) s.work.kind = kCutNone;
-        __syncthreads();
         return;
     }
-    double most;
-    uint32_t top;
-    if constexpr (DT == FSD_BF16) {
-        top = bin_prefix(top_bin);
-        most = one_value(top_bin) ? bin_value<DT>(top_bin) : 0.0;
-    } else {
+    if (mine.n != 0u) {
+        Run run = before;
+#pragma unroll
+        for (int j = 0; j < kBinsEach; ++j) {
+            const int place = tid * kBinsEach + j, bin = kBins - 1 - place;
+            if (n[j] != 0u) {
+                if (run.n == 0u) {
+                    s.found[1] = place;
+                    if (DT == FSD_BF16 && c.m && one_value(bin)) s.min_key = min_p_key<DT>(c.min_p, bin_prefix(bin), bin_value<DT>(bin));
+                }
+                if (cut_k && run.n < c.top_k && run.n + n[j] >= c.top_k) {
+                    s.found[0] = place;
+                    s.work.ties = c.top_k - run.n;
+                    s.goal = run.w + static_cast<double>(c.top_k - run.n) * w[j];
+                }
+            }
+            run.n += n[j];
+            run.w += bin == kBinTinyPos ? tiny : n[j] * w[j];
+        }
+    }
+    __syncthreads();
+    const int k_place = s.found[0], k_bin = kBins - 1 - k_place, top_bin = kBins - 1 - s.found[1];
+    uint32_t top = bin_prefix(top_bin);
+    double most = one_value(top_bin) ? bin_value<DT>(top_bin) : 0.0;
+    if constexpr (DT == FSD_F32) {
         top = 0u;
         for (int k = 0; k < blocks; ++k) top = top > s.top[k] ? top : s.top[k];
         most = value_of<FSD_F32>(top);
     }
     // Values off the bins: above them, or a border in a bin of many; below them what is worth nothing beside a highest value of
     // at least -60 (e^-68 of it each) and is nothing but a count.
-    if (hist[kBinOver] != 0u || !one_value(top_bin) || (hist[kBinUnder] != 0u && most < -60.0) || (cut_k && !one_value(k_bin))) {
-        if (tid == 0) s.work.kind = kCutByBits;
-        __syncthreads();
-        return;
-    }
-    // top-p: the first place at which the tokens so far weigh the goal
-    const double share = cut_k ? s.goal : all.w, goal = static_cast<double>(c.top_p) * share;
-    if (c.p) {
-        run = before;
+    const bool off = hist[kBinOver] != 0u || !one_value(top_bin) || (hist[kBinUnder] != 0u && most < -60.0) || (cut_k && !one_value(k_bin));
+    const double goal = static_cast<double>(c.top_p) * (cut_k ? s.goal : all.w);
+    int p_place = k_place;
+    if (c.p && !off) {                                       // the first place at which the tokens so far weigh the goal
+        int mine_at = kBins;
+        if (mine.n != 0u || tiny != 0.0) {
+            Run run = before;
 #pragma unroll
-        for (int j = 0; j < kBinsEach; ++j) {
-            const int place = tid * kBinsEach + j, bin = kBins - 1 - place;
-            run.w += bin == kBinTinyPos ? tiny : n[j] * w[j];
-            if (n[j] != 0u && run.w >= goal) { atomicMin(&s.found[2], place); break; }
+            for (int j = 0; j < kBinsEach; ++j) {
+                const int place = tid * kBinsEach + j, bin = kBins - 1 - place;
+                run.w += bin == kBinTinyPos ? tiny : n[j] * w[j];
+                if (n[j] != 0u && run.w >= goal && mine_at == kBins) mine_at = place;
+            }
         }
+        mine_at = __reduce_min_sync(0xffffffffu, mine_at);
+        if ((tid & 31) == 0 && mine_at < kBins) atomicMin(&s.found[2], mine_at);
         __syncthreads();
+        p_place = s.found[2];
+        if (cut_k && p_place > k_place) p_place = k_place;
+        if (!(goal > 0.0)) p_place = s.found[1];
+        if (p_place >= kBins) p_place = kBins - 1;           // (not reached: the goal is below the whole)
     }
-    int p_place = s.found[2];
-    if (cut_k && p_place > k_place) p_place = k_place;
-    if (c.p && !(goal > 0.0)) p_place = s.found[1];
-    if (p_place >= kBins) p_place = kBins - 1;              // (not reached: the goal is below the whole)
     const int p_bin = kBins - 1 - p_place;
-    if (c.p && !one_value(p_bin)) {
+    if (off || (c.p && !one_value(p_bin))) {
         if (tid == 0) s.work.kind = kCutByBits;
-        __syncthreads();
         return;
     }
     if constexpr (DT == FSD_BF16) {
-        // the thread that has the border's bin
-        if (c.p && p_place / kBinsEach == tid) {
-            run = before;
+        const bool has = (c.p || cut_k) && p_place / kBinsEach == tid;        // the thread that has the cut's bin
+        if (has) {
+            Run run = before;
 #pragma unroll
             for (int j = 0; j < kBinsEach; ++j) {
                 const int bin = kBins - 1 - (tid * kBinsEach + j);
                 if (bin == p_bin) {
-                    const long long t = ties_below(run.w, w[j], goal, V);
-                    const long long k_ties = s.work.ties;
-                    s.work.ties = cut_k && p_place == k_place && k_ties < t ? k_ties : t;
+                    const bool at_k = cut_k && p_place == k_place;
+                    long long t = c.p ? ties_below(run.w, w[j], goal, V) : V;
+                    if (at_k && s.work.ties < t) t = s.work.ties;
+                    s.work.ties = t >= n[j] ? V : t;                          // all of them
                     s.work.key = bin_prefix(bin);
-                    if (s.work.ties >= n[j]) s.work.ties = V;       // all of them
                 }
                 run.w += bin == kBinTinyPos ? tiny : n[j] * w[j];
             }
-        } else if (!c.p && cut_k && k_place / kBinsEach == tid) {
+        }
+        if (has || (!c.p && !cut_k && tid == 0)) {
+            if (s.min_key > s.work.key) { s.work.key = s.min_key; s.work.ties = V; }
+            if (s.work.key == 0u) s.work.kind = kCutNone;
+        }
+    } else if (tid == 0) {
+        s.found[3] = p_bin;
+        if (cut_k) {
+            s.work.kind = kCutRefineK;
             s.work.key = bin_prefix(k_bin);
-            if (s.work.ties >= hist[k_bin]) s.work.ties = V;
-        }
-        __syncthreads();
-        if (tid < 32) {
-            const uint32_t t = c.m ? min_p_key<DT>(c.min_p, top, most) : 0u;
-            if (tid == 0 && t > s.work.key) { s.work.key = t; s.work.ties = V; }
-            if (tid == 0 && s.work.key == 0u) s.work.kind = kCutNone;
-        }
-    } else {
-        const uint32_t t = tid < 32 && c.m && !cut_k && !c.p ? min_p_key<DT>(c.min_p, top, most) : 0u;
-        if (tid == 0) {
-            s.found[3] = p_bin;
-            if (cut_k) {
-                s.work.kind = kCutRefineK;
-                s.work.key = bin_prefix(k_bin);
-            } else if (c.p) {
-                s.work.kind = kCutRefineP;
-                s.work.key = bin_prefix(p_bin);
-            } else if (c.m) {
-                s.work.key = t;
-            } else {
-                s.work.kind = kCutNone;                     // (fewer tokens than top_k)
-            }
+        } else if (c.p) {
+            s.work.kind = kCutRefineP;
+            s.work.key = bin_prefix(p_bin);
+        } else if (c.m) {
+            s.work.key = min_p_key<DT>(c.min_p, top, most);
+        } else {
+            s.work.kind = kCutNone;                          // (fewer tokens than top_k)
         }
     }
-    __syncthreads();
 }
 
 // Counts, by the 8 bits above `shift`, the tokens whose keys have the upper bits `prefix` and are above `over`; with weights also
@@ -448,7 +492,7 @@ __device__ void count_bits(const RowSlice<FSD_F32>& row, CutShared& s, CutShared
             const uint32_t k = key_of<FSD_F32>(bits[e]), high = k >> (shift + 8);
             if (WEIGHTS && bits[e] != 0xff800000u && k > over) {
                 if (high != prefix) {
-                    const double w = exp(static_cast<double>(__uint_as_float(bits[e])) - most);
+                    const double w = exp_of(static_cast<double>(__uint_as_float(bits[e])) - most);
                     if (high > prefix) above.w += w; else rest.w += w;
                 }
             }
@@ -457,7 +501,7 @@ __device__ void count_bits(const RowSlice<FSD_F32>& row, CutShared& s, CutShared
                 atomicAdd(&s.sub_n[bin], 1u);
                 if (WEIGHTS)
                     atomicAdd(reinterpret_cast<unsigned long long*>(&s.sub_w[bin]),
-                              static_cast<unsigned long long>(__double2ull_rn(exp(static_cast<double>(__uint_as_float(bits[e])) - edge) * kFixed)));
+                              __double2ull_rn(exp_of(static_cast<double>(__uint_as_float(bits[e])) - edge) * kFixed));
             }
         }
     }
@@ -504,9 +548,9 @@ __device__ __forceinline__ int next_bin(const uint32_t* hist, CutShared& s, int 
     return found == kBins ? -1 : found;
 }
 
-__device__ __forceinline__ void at_least_min_p(CutShared& s, const CutParams& c, int V, uint32_t top) {       // one warp
+__device__ __forceinline__ void at_least_min_p(CutShared& s, const CutParams& c, int V, uint32_t top) {       // one thread
     const uint32_t t = min_p_key<FSD_F32>(c.min_p, top, value_of<FSD_F32>(top));
-    if (threadIdx.x == 0 && t > s.work.key) { s.work.key = t; s.work.ties = V; }
+    if (t > s.work.key) { s.work.key = t; s.work.ties = V; }
 }
 
 // fp32: from the bins of the cuts to the cuts.
@@ -521,21 +565,19 @@ __device__ CutResult refine(const RowSlice<FSD_F32>& row, const uint32_t* hist, 
             count_bits<false>(row, s, first, rank, res.key, shift, 0u, most);
             cluster_barrier();
             if (rank == 0) {
-                CountAndWeight all;
+                Run all;
                 const int bin = 255 - tid;
-                const long long n = tid < 256 ? s.sub_n[bin] : 0;
-                const CountAndWeight before = scan_threads({n, 0.0}, s.scratch, all);
+                const uint32_t n = tid < 256 ? s.sub_n[bin] : 0u;
+                const Run before = scan_threads({n, 0.0}, s, all);
                 if (before.n < res.ties && before.n + n >= res.ties) {
                     s.work.key = res.key << 8 | static_cast<uint32_t>(bin);
                     s.work.ties = res.ties - before.n;
                     if (shift == 0) s.work.over = s.work.ties >= n;            // whether all that are equal are kept
                 }
                 __syncthreads();
-                if (tid < 32 && shift == 0 && !c.p) {
-                    if (tid == 0) {
-                        s.work.kind = kCutDone;
-                        if (s.work.over) s.work.ties = V;
-                    }
+                if (tid == 0 && shift == 0 && !c.p) {
+                    s.work.kind = kCutDone;
+                    if (s.work.over) s.work.ties = V;
                     if (c.m) at_least_min_p(s, c, V, top);
                 }
             }
@@ -547,7 +589,7 @@ __device__ CutResult refine(const RowSlice<FSD_F32>& row, const uint32_t* hist, 
     const uint32_t over = cut_k ? res.key : 0u;
     const long long k_ties = cut_k ? res.ties : 0;
     const bool all_of_k = cut_k && res.over;
-    const double of_ties = cut_k ? static_cast<double>(k_ties) * exp_d(static_cast<double>(value_of<FSD_F32>(over)) - most) : 0.0;
+    const double of_ties = cut_k ? static_cast<double>(k_ties) * exp_of(static_cast<double>(value_of<FSD_F32>(over)) - most) : 0.0;
     if (cut_k) {
         if (rank == 0 && tid == 0) s.work = {kCutRefineP, bin_prefix(p_bin), 0, 0u};
         res = tell_result(s, cluster, rank, blocks, turn);
@@ -562,12 +604,12 @@ __device__ CutResult refine(const RowSlice<FSD_F32>& row, const uint32_t* hist, 
         if (rank == 0) {
             double above = 0.0, rest = 0.0;
             for (int k = 0; k < blocks; ++k) { above += s.above[k]; rest += s.rest[k]; }
-            const double unit = exp_d(static_cast<double>(value_of<FSD_F32>(prefix << 16 | 0xffffu)) - most) / kFixed;
-            CountAndWeight all;
+            const double unit = exp_of(static_cast<double>(value_of<FSD_F32>(prefix << 16 | 0xffffu)) - most) / kFixed;
+            Run all;
             const int bin = 255 - tid;
             const double w = tid < 256 ? static_cast<double>(s.sub_w[bin]) * unit : 0.0;
-            const long long n = tid < 256 ? s.sub_n[bin] : 0;
-            const CountAndWeight before = scan_threads({n, w}, s.scratch, all);
+            const uint32_t n = tid < 256 ? s.sub_n[bin] : 0u;
+            const Run before = scan_threads({n, w}, s, all);
             const double goal = static_cast<double>(c.top_p) * (above + all.w + rest + of_ties);
             if (tid == 0) { s.found[1] = -1; s.found[2] = 256; }
             __syncthreads();
@@ -606,12 +648,12 @@ __device__ CutResult refine(const RowSlice<FSD_F32>& row, const uint32_t* hist, 
         count_bits<false>(row, s, first, rank, prefix, 0, over, most);
         cluster_barrier();
         if (rank == 0) {
-            CountAndWeight all;
+            Run all;
             const int bin = 255 - tid;
             const uint32_t key = prefix << 8 | static_cast<uint32_t>(bin);
-            const long long n = tid < 256 ? s.sub_n[bin] : 0;
-            const double w = n != 0 ? exp_d(static_cast<double>(value_of<FSD_F32>(key)) - most) : 0.0;
-            const CountAndWeight before = scan_threads({n, static_cast<double>(n) * w}, s.scratch, all);
+            const uint32_t n = tid < 256 ? s.sub_n[bin] : 0u;
+            const double w = n != 0 ? exp_of(static_cast<double>(value_of<FSD_F32>(key)) - most) : 0.0;
+            const Run before = scan_threads({n, static_cast<double>(n) * w}, s, all);
             if (tid == 0) s.found[2] = 256;
             __syncthreads();
             // (where rounding leaves the last of them short of the goal it is the border all the same)
@@ -625,7 +667,7 @@ __device__ CutResult refine(const RowSlice<FSD_F32>& row, const uint32_t* hist, 
         }
     }
     if (res.kind != kCutByBits && (res.kind == kCutRefineK || c.m)) {
-        if (rank == 0 && tid < 32 && c.m) at_least_min_p(s, c, V, top);
+        if (rank == 0 && tid == 0 && c.m) at_least_min_p(s, c, V, top);
         res = tell_result(s, cluster, rank, blocks, turn);
     }
     return res;
@@ -650,7 +692,9 @@ __device__ __noinline__ double count_value(uint32_t bits, uint32_t* hist) {
     int bin = static_cast<int>(u ^ static_cast<uint32_t>(static_cast<int>(bits) >> 31)) + kHalfBins;
     if ((bits & 0x7fffffffu) > 0x7f800000u) bin = kBinOver;
     atomicAdd(&hist[bin], static_cast<uint32_t>(BY));
-    return u != 0u ? 0.0 : (bits & 0x7fffffffu) == 0u ? 1.0 : exp(static_cast<double>(__uint_as_float(bits)));
+    if (u != 0u) return 0.0;
+    const double y = static_cast<double>(__uint_as_float(bits));                  // below 2^-8: the series up to y^6 / 720 (y^7 / 5040 < 3e-21)
+    return 1.0 + y * (1.0 + y * (1.0 / 2.0 + y * (1.0 / 6.0 + y * (1.0 / 24.0 + y * (1.0 / 120.0 + y * (1.0 / 720.0))))));
 }
 // A vector of values, which `kept` has too, into the bins; returns what is weighed.  bf16: two at a time, in halves of a word.
 template <int DT>
@@ -765,14 +809,31 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_kernel(const ProcArgs 
     const int row_vecs = (a.V + lies + N - 1) / N, v0 = rank * slice;
     RowSlice<DT> row = {on_chip, row_vecs - v0 < slice ? (row_vecs > v0 ? row_vecs - v0 : 0) : slice, v0 * N - lies};
 
-    const CutParams c = cut_params(a, b);
-    const bool cutting = c.k || c.p || c.m;
-    const SeqParams p = seq_params(a, b);
+    constexpr int kAtOnce = 4;
+    uint4 got[kAtOnce];
+    const auto fetch = [&](int i0) {
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int i = i0 + u * kRowThreads, t0 = row.first + i * N;
+            if (i < row.n) got[u] = load_ids<DT>(in, t0, a.V, t0 >= 0 && t0 + N <= a.V);
+        }
+    };
+    fetch(tid);
+    if (tid < 8) {                                          // the sequence's settings, all read at once
+        const void* const at_b[8] = {a.top_k, a.top_p, a.min_p, a.repetition, a.frequency, a.presence, a.temperature, nullptr};
+        const void* from = nullptr;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) from = k == tid ? at_b[k] : from;
+        s.settings[tid] = from != nullptr ? __ldg(static_cast<const uint32_t*>(from) + b) : tid == 1 || tid == 3 ? 0x3f800000u : 0u;
+    }
     const int ctx = context_row(a, b, side, r);
     const int drafts = !raw && a.penalties && a.tokens != nullptr ? a.P : 0;
+    const bool history = !raw && a.penalties && a.seen != nullptr;
+    const uint32_t* seen = history ? a.seen + static_cast<size_t>(b) * a.W : nullptr;
+    const uint32_t* allowed = !raw && a.allowed != nullptr ? a.allowed + (static_cast<size_t>(b) * (a.P + 1) + ctx) * a.W : nullptr;
     const int ids_lo = row.first > 0 ? row.first : 0, ids_hi = row.first + row.n * N < a.V ? row.first + row.n * N : a.V;   // of the slice
-    const int word0 = ids_lo >> 5, n_words = ids_hi > ids_lo ? (ids_hi + 31 >> 5) - word0 : 0;
-    for (int i = tid; i < kBins; i += kRowThreads) hist[i] = 0u;
+    const int word0 = ids_lo >> 5, n_words = ids_hi > ids_lo ? ((ids_hi + 31) >> 5) - word0 : 0;
+    for (int i = tid; i < kBins / 4; i += kRowThreads) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0u, 0u, 0u, 0u);
     if (drafts > 0)
         for (int i = tid; i < n_words; i += kRowThreads) drafted_ids[i] = 0u;
     if (tid < 256) { s.sub_n[tid] = 0u; s.sub_w[tid] = 0u; }
@@ -782,43 +843,47 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_kernel(const ProcArgs 
         const int t = __ldg(a.tokens + static_cast<size_t>(b) * a.P + j);
         if (t >= ids_lo && t < ids_hi) atomicOr(&drafted_ids[(t >> 5) - word0], 1u << (t & 31));
     }
-    const bool history = !raw && a.penalties && a.seen != nullptr;
-    const uint32_t* seen = history ? a.seen + static_cast<size_t>(b) * a.W : nullptr;
-    const uint32_t* allowed = !raw && a.allowed != nullptr ? a.allowed + (static_cast<size_t>(b) * (a.P + 1) + ctx) * a.W : nullptr;
+    const CutParams c = cut_params(s.settings, a.V);
+    const bool cutting = c.k || c.p || c.m;
+    const SeqParams p = seq_params(s.settings + 3);
 
     // the slice: read, processed, counted, kept
     double tiny = 0.0;
     uint32_t top = 0u;
-#pragma unroll 2
-    for (int i = tid; i < row.n; i += kRowThreads) {
-        const int t0 = row.first + i * N;
-        const bool whole = t0 >= 0 && t0 + N <= a.V;
-        uint4 v = load_ids<DT>(in, t0, a.V, whole);
-        if (!raw) {
-            uint32_t may = allowed != nullptr ? bits8(allowed, t0, 4 * a.W) : 0xffu;
-            if (!whole) may &= ids_of<N>(t0, a.V);              // (what is not in the row counts as masked)
-            v = process_vec<DT>(v, may, p.inv_temp);
-        }
-        row.vecs[i] = v;
-        if (!cutting) continue;
-        tiny += count_vec<DT>(v, row.vecs + i, hist);
-        if constexpr (DT == FSD_F32) {
-            const uint32_t bits[4] = {v.x, v.y, v.z, v.w};
-            const uint32_t sparse = (history ? bits8(seen, t0, 4 * a.W) : 0u) | (drafts > 0 ? bits8(drafted_ids, t0 - word0 * 32, 4 * n_words) : 0u);
+    for (int i0 = tid; i0 < row.n; i0 += kAtOnce * kRowThreads) {
+        if (i0 != tid) fetch(i0);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t k = key_of<DT>(bits[e]);
-                if (!(sparse >> e & 1u)) top = top > k ? top : k;
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int i = i0 + u * kRowThreads, t0 = row.first + i * N;
+            if (i >= row.n) break;
+            uint4 v = got[u];
+            if (!raw) {
+                uint32_t may = allowed != nullptr ? bits8(allowed, t0, 4 * a.W) : 0xffu;
+                if (t0 < 0 || t0 + N > a.V) may &= ids_of<N>(t0, a.V);        // (what is not in the row counts as masked)
+                v = process_vec<DT>(v, may, p.inv_temp);
+            }
+            row.vecs[i] = v;
+            if (!cutting) continue;
+            tiny += count_vec<DT>(v, row.vecs + i, hist);
+            if constexpr (DT == FSD_F32) {
+                const uint32_t bits[4] = {v.x, v.y, v.z, v.w};
+                const uint32_t sparse = (history ? bits8(seen, t0, 4 * a.W) : 0u) | (drafts > 0 ? bits8(drafted_ids, t0 - word0 * 32, 4 * n_words) : 0u);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t k = key_of<DT>(bits[e]);
+                    if (!(sparse >> e & 1u)) top = top > k ? top : k;
+                }
             }
         }
     }
     // Then the ids that are used or drafted, one a thread: what was counted for them without a penalty is taken back.  A warp takes
-    // 32 words of the bitmaps at a time and lists their bits, so that its threads have as many each.
+    // 32 words of the bitmaps at a time, each kRowWarps from the last (low ids are used far more often), and lists their bits,
+    // so that its threads have as many each.
     if (history || drafts > 0) {
         __syncthreads();
         LogitWord<DT>* words = reinterpret_cast<LogitWord<DT>*>(row.vecs) - row.first;      // by id
-        for (int w0 = warp * 32; w0 < n_words; w0 += kRowWarps * 32) {
-            const int w = w0 + lane;
+        for (int w0 = warp; w0 < n_words; w0 += kRowWarps * 32) {
+            const int w = w0 + lane * kRowWarps;
             uint32_t used = 0u, draft = 0u;
             if (w < n_words) {
                 uint32_t may = allowed != nullptr ? allowed[word0 + w] : 0xffffffffu;
@@ -845,13 +910,13 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_kernel(const ProcArgs 
                 }
                 __syncwarp();
                 const int n = total - base < 256 ? total - base : 256;
-#pragma unroll 2
+#pragma unroll 4
                 for (int k0 = 0; k0 < n; k0 += 32) {
                     const int k = k0 + lane, l = k < n ? s.list[warp][k] : 0;
                     const uint32_t is_used = __shfl_sync(0xffffffffu, used, l >> 5) >> (l & 31) & 1u;
                     const uint32_t is_draft = __shfl_sync(0xffffffffu, draft, l >> 5) >> (l & 31) & 1u;
                     if (k >= n) continue;
-                    const int t = (word0 + w0) * 32 + l;
+                    const int t = (word0 + w0 + (l >> 5) * kRowWarps) * 32 + (l & 31);
                     const int count = is_used ? __ldg(a.counts + static_cast<size_t>(b) * a.V + t) : -1;
                     const float x = read_id<DT>(in, t);
                     const int d = is_draft ? drafted(a, b, ctx, t) : 0;
@@ -877,14 +942,27 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_kernel(const ProcArgs 
     }
 
     CutShared& first = *cluster.map_shared_rank(&s, 0);
-    const CountAndWeight tiny_all = block_total({0, tiny}, s.scratch);
-    if constexpr (DT == FSD_F32) top = block_largest(top, s.scratch);
+    if (__any_sync(0xffffffffu, tiny != 0.0)) tiny = warp_sum(tiny);
+    if constexpr (DT == FSD_F32) top = __reduce_max_sync(0xffffffffu, top);
+    if (lane == 0) { s.warp_w[warp] = tiny; s.warp_n[warp] = top; }
+    __syncthreads();
     cluster_wait();
-    if (tid == 0) { first.tiny[rank] = tiny_all.w; first.top[rank] = top; }
+    if (tid == 0) {
+        tiny = 0.0;
+#pragma unroll
+        for (int w = 0; w < kRowWarps; ++w) { tiny += s.warp_w[w]; top = top > s.warp_n[w] ? top : s.warp_n[w]; }
+        first.tiny[rank] = tiny;
+        first.top[rank] = top;
+    }
     if (rank != 0) {
         uint32_t* sums = cluster.map_shared_rank(hist, 0);
-        for (int i = tid; i < kBins; i += kRowThreads)
-            if (hist[i] != 0u) atomicAdd(sums + i, hist[i]);
+        for (int i = tid; i < kBins / 4; i += kRowThreads) {
+            const uint4 v = reinterpret_cast<const uint4*>(hist)[i];
+            if (v.x != 0u) atomicAdd(sums + 4 * i, v.x);
+            if (v.y != 0u) atomicAdd(sums + 4 * i + 1, v.y);
+            if (v.z != 0u) atomicAdd(sums + 4 * i + 2, v.z);
+            if (v.w != 0u) atomicAdd(sums + 4 * i + 3, v.w);
+        }
     }
     cluster_barrier();
     if (rank == 0) {
