@@ -64,6 +64,22 @@ CutShape cut_shape(const ProcArgs& a, bool raw) {
     return c;
 }
 
+// bf16: whether a block does a row by itself, and its shared memory: the bins, and where there are sparse ids their bitmap and list, of 8192
+// of them if two blocks an SM have room for it.
+bool rows_shape(const ProcArgs& a, bool raw, RowsShape* shape, size_t* smem) {
+    const bool sparse = !raw && a.penalties && (a.seen != nullptr || a.tokens != nullptr);
+    shape->words = sparse ? (a.W + 3) / 4 * 4 : 0;
+    shape->cap = 0;
+    const size_t fixed = kBins * sizeof(uint32_t) + static_cast<size_t>(shape->words) * 6;
+    if (sparse) {
+        const long long room = (fixed < 90 * 1024 ? 94 * 1024ll : 190 * 1024ll) - static_cast<long long>(fixed);
+        if (room < 6 * 256) return false;
+        shape->cap = static_cast<int>(room / 6 < 8192 ? room / 6 / 8 * 8 : 8192);
+    }
+    *smem = fixed + static_cast<size_t>(shape->cap) * 6;
+    return true;
+}
+
 // Rows that are cut off: a cluster of blocks holds a row in shared memory where it fits, else a block sweeps over it in memory.
 template <int DT>
 int launch_cut(const ProcArgs& a, bool raw, cudaStream_t s) {
@@ -76,7 +92,20 @@ int launch_cut(const ProcArgs& a, bool raw, cudaStream_t s) {
         std::lock_guard<std::mutex> lock(mu);
         if (!ready[dev]) {
             if (cudaFuncSetAttribute(fsd_cut_kernel<DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kCutSmem)) != cudaSuccess) return FSD_ERR_CUDA;
+            if (DT == FSD_BF16 && cudaFuncSetAttribute(fsd_cut_rows_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kCutSmem)) != cudaSuccess)
+                return FSD_ERR_CUDA;
+            static double weights[kBins];                 // (under the lock)
+            fill_bin_weights(weights);
+            if (cudaMemcpyToSymbol(bin_weights, weights, sizeof weights) != cudaSuccess) return FSD_ERR_CUDA;
             ready[dev] = true;
+        }
+    }
+    if constexpr (DT == FSD_BF16) {
+        RowsShape shape;
+        size_t smem;
+        if (rows_shape(a, raw, &shape, &smem)) {
+            fsd_cut_rows_kernel<<<static_cast<unsigned>(a.B) * (a.rows[0] + a.rows[1]), kRowThreads, smem, s>>>(a, shape, raw);
+            return cudaGetLastError() == cudaSuccess ? FSD_OK : FSD_ERR_CUDA;
         }
     }
     const CutShape c = cut_shape<DT>(a, raw);
@@ -102,8 +131,11 @@ int launch_cut(const ProcArgs& a, bool raw, cudaStream_t s) {
 template <int DT>
 int launch(const ProcArgs& a, bool cut, cudaStream_t s) {
     const int all = a.rows[0] + a.rows[1];
-    // The cut kernel does the rest too where the row stays on chip and there are no biases (whose lookup wants room there).
-    if (cut && a.bias_offsets == nullptr && cut_shape<DT>(a, false).fits) return launch_cut<DT>(a, false, s);
+    // The cut kernel does the rest too where it has room for it and there are no biases (whose lookup wants room there).
+    RowsShape shape;
+    size_t smem;
+    const bool room = DT == FSD_BF16 ? rows_shape(a, false, &shape, &smem) : cut_shape<DT>(a, false).fits;
+    if (cut && a.bias_offsets == nullptr && room) return launch_cut<DT>(a, false, s);
     // a row's vectors, wherever it starts, by blocks
     const long long spans = (a.V + 2 * (Logit<DT>::kPerVec - 1)) / Logit<DT>::kPerVec / kProcThreads + 1;
     // as many rows a block as leave eight blocks an SM, so that the counts are read for many rows at once

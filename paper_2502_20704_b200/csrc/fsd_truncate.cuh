@@ -5,6 +5,9 @@
 // whole in a flat row of 150000: sums are in double precision, and whether two programs agree never hangs on their order.
 #pragma once
 
+#include <climits>
+#include <cmath>
+#include <cstring>
 #include <cuda_bf16.h>
 #include <type_traits>
 
@@ -246,7 +249,7 @@ constexpr uint32_t kMagLo = 0x3b7f, kMagHi = 0x4300;       // upper halves: just
 constexpr int kHalfBins = static_cast<int>(kMagHi - kMagLo) + 1;
 constexpr int kBins = 2 * kHalfBins;                       // negative magnitudes falling, then positive ones rising
 constexpr int kBinUnder = 0, kBinOver = kBins - 1, kBinTinyNeg = kHalfBins - 1, kBinTinyPos = kHalfBins;
-constexpr int kBinsEach = (kBins + kRowThreads - 1) / kRowThreads;
+constexpr int kBinsEach = ((kBins + kRowThreads - 1) / kRowThreads + 3) / 4 * 4;
 constexpr double kFixed = 4398046511104.0;                 // 2^42: weights of a bin's tokens as whole numbers
 
 // The upper 16 bits of the keys of a one-value bin, and back.
@@ -254,6 +257,10 @@ __device__ __forceinline__ uint32_t bin_prefix(int bin) {
     return bin >= kHalfBins ? 0x8000u | (kMagLo + static_cast<uint32_t>(bin - kHalfBins)) : 0x7fffu ^ (kMagLo + static_cast<uint32_t>(kHalfBins - 1 - bin));
 }
 __device__ __forceinline__ bool one_value(int bin) { return bin != kBinUnder && bin != kBinOver && bin != kBinTinyNeg && bin != kBinTinyPos; }
+__device__ __forceinline__ int bin_of_value(float y) {      // one of a one-value bin
+    const uint32_t bits = __float_as_uint(y), u = (bits >> 16 & 0x7fffu) - kMagLo;
+    return static_cast<int>(u ^ static_cast<uint32_t>(static_cast<int>(bits) >> 31)) + kHalfBins;
+}
 // The value of a bin: bf16 its only one, fp32 the middle of its range.
 template <int DT>
 __device__ __forceinline__ double bin_value(int bin) {
@@ -261,12 +268,27 @@ __device__ __forceinline__ double bin_value(int bin) {
     else return value_of<FSD_F32>(bin_prefix(bin) << 16 | 0x8000u);
 }
 
+// exp of every bin's value by place, from the highest bin down, and 0 for bins of many values.  The host fills it in front of a
+// device's first call; worked out where it is needed it took the first block 2000 cycles a row.
+__device__ __align__(16) double bin_weights[kBins];
+inline void fill_bin_weights(double* w) {
+    for (int k = 0; k < kBins; ++k) w[k] = 0.0;
+    for (int u = 1; u < kHalfBins - 1; ++u) {
+        const uint32_t bits = (kMagLo + static_cast<uint32_t>(u)) << 16;
+        float v;
+        memcpy(&v, &bits, 4);
+        w[kBins - 1 - (kHalfBins + u)] = ::exp(static_cast<double>(v));
+        w[kBins - 1 - (kHalfBins - 1 - u)] = ::exp(-static_cast<double>(v));
+    }
+}
+
 enum CutKind { kCutNone, kCutDone, kCutByBits, kCutRefineK, kCutRefineP };
 struct CutResult {
     int kind;
     uint32_t key;              // of the cut; while it is being refined, its upper bits
     long long ties;
-    uint32_t over;             // refining top-p: the tokens above this key are in the top_k
+    uint32_t over;             // refining top-k: whether all that are equal to the k-th are kept
+    uint32_t equal;            // bf16: how many tokens are equal to the cut
 };
 struct CutShared {
     double tiny[kMaxCutCluster], above[kMaxCutCluster], rest[kMaxCutCluster];
@@ -284,7 +306,6 @@ struct CutShared {
     CutResult told[2];         // what the first block told last, and the time before
     int found[4];
     double goal, above_goal;
-    int warp_equal[kRowWarps + 1];
     uint16_t list[kRowWarps][256];
 };
 
@@ -340,7 +361,7 @@ __device__ __forceinline__ void solve_bins(const uint32_t* hist, CutShared& s, c
     if (tid == 0) {
         s.found[0] = -1;                                     // place of the k-th token
         s.found[1] = s.found[2] = kBins;                     // of the highest one, and of the border of top-p
-        s.work = {kCutDone, 0u, V, 0u};
+        s.work = {kCutDone, 0u, V, 0u, 0u};
         s.min_key = 0u;
     }
     uint32_t n[kBinsEach];
@@ -362,12 +383,13 @@ __device__ __forceinline__ void solve_bins(const uint32_t* hist, CutShared& s, c
 #pragma unroll
     for (int j = 0; j < kBinsEach; ++j) w[j] = 0.0;
     if (mine.n != 0u) {
+        // (fp32: as if all of a bin were at its edge next to zero)
+        const double2* table = reinterpret_cast<const double2*>(bin_weights + tid * kBinsEach);
 #pragma unroll
-        for (int j = 0; j < kBinsEach; ++j) {
-            const int bin = kBins - 1 - (tid * kBinsEach + j);
-            w[j] = one_value(bin) ? exp_of(bin_value<DT>(bin)) : 0.0;
-            mine.w += n[j] * w[j];
-        }
+        for (int j = 0; j < kBinsEach; j += 2)
+            if (tid * kBinsEach + j < kBins) { const double2 t = __ldg(table + j / 2); w[j] = t.x; w[j + 1] = t.y; }
+#pragma unroll
+        for (int j = 0; j < kBinsEach; ++j) mine.w += n[j] * w[j];
     }
     mine.w += tiny;
     Run all;
@@ -413,7 +435,7 @@ __device__ __forceinline__ void solve_bins(const uint32_t* hist, CutShared& s, c
     int p_place = k_place;
     if (c.p && !off) {                                       // the first place at which the tokens so far weigh the goal
         int mine_at = kBins;
-        if (mine.n != 0u || tiny != 0.0) {
+        if ((mine.n != 0u || tiny != 0.0) && !(before.w + mine.w < goal * (1.0 - 1e-9)) && before.w < goal) {      // (rounded in another order)
             Run run = before;
 #pragma unroll
             for (int j = 0; j < kBinsEach; ++j) {
@@ -428,7 +450,15 @@ __device__ __forceinline__ void solve_bins(const uint32_t* hist, CutShared& s, c
         p_place = s.found[2];
         if (cut_k && p_place > k_place) p_place = k_place;
         if (!(goal > 0.0)) p_place = s.found[1];
-        if (p_place >= kBins) p_place = kBins - 1;           // (not reached: the goal is below the whole)
+        if (p_place >= kBins) {                              // where two threads' sums meet: the first that starts at the goal
+            mine_at = __reduce_min_sync(0xffffffffu, mine.n != 0u && before.w >= goal ? tid * kBinsEach : kBins);
+            if ((tid & 31) == 0 && mine_at < kBins) atomicMin(&s.found[2], mine_at);
+            __syncthreads();
+            p_place = s.found[2];
+            while (p_place < kBins && hist[kBins - 1 - p_place] == 0u) ++p_place;
+            if (cut_k && p_place > k_place) p_place = k_place;
+            if (p_place >= kBins) p_place = kBins - 1;       // (not reached: the goal is below the whole)
+        }
     }
     const int p_bin = kBins - 1 - p_place;
     if (off || (c.p && !one_value(p_bin))) {
@@ -447,6 +477,7 @@ __device__ __forceinline__ void solve_bins(const uint32_t* hist, CutShared& s, c
                     long long t = c.p ? ties_below(run.w, w[j], goal, V) : V;
                     if (at_k && s.work.ties < t) t = s.work.ties;
                     s.work.ties = t >= n[j] ? V : t;                          // all of them
+                    s.work.equal = n[j];
                     s.work.key = bin_prefix(bin);
                 }
                 run.w += bin == kBinTinyPos ? tiny : n[j] * w[j];
@@ -521,13 +552,14 @@ __device__ void count_bits(const RowSlice<FSD_F32>& row, CutShared& s, CutShared
 
 // The first block tells the others what it found, and clears the counts for the next time.  Two places in turn: a block may still
 // be reading what it was told before.
-__device__ __forceinline__ CutResult tell_result(CutShared& s, cg::cluster_group& cluster, int rank, int blocks, int& turn) {
+__device__ __forceinline__ CutResult tell_result(CutShared& s, cg::cluster_group& cluster, int rank, int blocks, int& turn, bool clear = true) {
     turn ^= 1;
     if (rank == 0) {
         const int tid = threadIdx.x;
         __syncthreads();
         if (tid < blocks) *cluster.map_shared_rank(&s.told[turn], tid) = s.work;
-        for (int i = tid; i < 256; i += kRowThreads) { s.sub_n[i] = 0u; s.sub_w[i] = 0u; }
+        if (clear)
+            for (int i = tid; i < 256; i += kRowThreads) { s.sub_n[i] = 0u; s.sub_w[i] = 0u; }
     }
     cluster_barrier();
     return s.told[turn];
@@ -591,7 +623,7 @@ __device__ CutResult refine(const RowSlice<FSD_F32>& row, const uint32_t* hist, 
     const bool all_of_k = cut_k && res.over;
     const double of_ties = cut_k ? static_cast<double>(k_ties) * exp_of(static_cast<double>(value_of<FSD_F32>(over)) - most) : 0.0;
     if (cut_k) {
-        if (rank == 0 && tid == 0) s.work = {kCutRefineP, bin_prefix(p_bin), 0, 0u};
+        if (rank == 0 && tid == 0) s.work = {kCutRefineP, bin_prefix(p_bin), 0, 0u, 0u};
         res = tell_result(s, cluster, rank, blocks, turn);
     }
     // The bin is a guess, made with the middles of the bins; the sums say whether to move to the next one in use.  (Where rounding would
@@ -625,7 +657,7 @@ __device__ CutResult refine(const RowSlice<FSD_F32>& row, const uint32_t* hist, 
             if (down && cut_k && prefix <= over >> 16) {                          // the border is among the tokens equal to the k-th
                 if (tid == 0) {
                     const long long t = ties_below(above + all.w, of_ties / static_cast<double>(k_ties), goal, V);
-                    s.work = {kCutDone, over, t < k_ties ? t : all_of_k ? V : k_ties, 0u};
+                    s.work = {kCutDone, over, t < k_ties ? t : all_of_k ? V : k_ties, 0u, 0u};
                 }
             } else if (up || down) {
                 p_bin = next_bin(hist, s, p_bin, up);
@@ -661,7 +693,7 @@ __device__ CutResult refine(const RowSlice<FSD_F32>& row, const uint32_t* hist, 
             __syncthreads();
             if (tid == s.found[2]) {
                 const long long t = ties_below(s.above_goal + before.w, w, s.goal, V);
-                s.work = {kCutDone, key, t >= n ? V : t, 0u};
+                s.work = {kCutDone, key, t >= n ? V : t, 0u, 0u};
             }
             __syncthreads();
         }
@@ -696,9 +728,9 @@ __device__ __noinline__ double count_value(uint32_t bits, uint32_t* hist) {
     const double y = static_cast<double>(__uint_as_float(bits));                  // below 2^-8: the series up to y^6 / 720 (y^7 / 5040 < 3e-21)
     return 1.0 + y * (1.0 + y * (1.0 / 2.0 + y * (1.0 / 6.0 + y * (1.0 / 24.0 + y * (1.0 / 120.0 + y * (1.0 / 720.0))))));
 }
-// A vector of values, which `kept` has too, into the bins; returns what is weighed.  bf16: two at a time, in halves of a word.
+// A vector of values into the bins; returns what is weighed.  bf16: two at a time, in halves of a word.
 template <int DT>
-__device__ __forceinline__ double count_vec(const uint4& v, const uint4* kept, uint32_t* hist) {
+__device__ __forceinline__ double count_vec(const uint4& v, uint32_t* hist) {
     double tiny = 0.0;
     if constexpr (DT == FSD_BF16) {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -714,7 +746,10 @@ __device__ __forceinline__ double count_vec(const uint4& v, const uint4* kept, u
         }
         if ((lowest & 0xffffu) == kMagLo || lowest >> 16 == kMagLo || (highest & 0xffffu) == kMagHi || highest >> 16 == kMagHi) {
 #pragma unroll 1
-            for (int e = 0; e < 8; ++e) tiny += count_value<1>(static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(kept)[e]) << 16, hist);
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t two = k < 2 ? (k < 1 ? v.x : v.y) : (k < 3 ? v.z : v.w);
+                tiny += count_value<1>(two << 16, hist) + count_value<1>(two & 0xffff0000u, hist);
+            }
         } else {
             uint32_t* mid = hist + kHalfBins;
 #pragma unroll
@@ -818,14 +853,15 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_kernel(const ProcArgs 
             if (i < row.n) got[u] = load_ids<DT>(in, t0, a.V, t0 >= 0 && t0 + N <= a.V);
         }
     };
-    fetch(tid);
+    uint32_t setting = 0u;
     if (tid < 8) {                                          // the sequence's settings, all read at once
         const void* const at_b[8] = {a.top_k, a.top_p, a.min_p, a.repetition, a.frequency, a.presence, a.temperature, nullptr};
         const void* from = nullptr;
 #pragma unroll
         for (int k = 0; k < 8; ++k) from = k == tid ? at_b[k] : from;
-        s.settings[tid] = from != nullptr ? __ldg(static_cast<const uint32_t*>(from) + b) : tid == 1 || tid == 3 ? 0x3f800000u : 0u;
+        setting = from != nullptr ? __ldg(static_cast<const uint32_t*>(from) + b) : tid == 1 || tid == 3 ? 0x3f800000u : 0u;
     }
+    fetch(tid);
     const int ctx = context_row(a, b, side, r);
     const int drafts = !raw && a.penalties && a.tokens != nullptr ? a.P : 0;
     const bool history = !raw && a.penalties && a.seen != nullptr;
@@ -836,7 +872,9 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_kernel(const ProcArgs 
     for (int i = tid; i < kBins / 4; i += kRowThreads) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0u, 0u, 0u, 0u);
     if (drafts > 0)
         for (int i = tid; i < n_words; i += kRowThreads) drafted_ids[i] = 0u;
-    if (tid < 256) { s.sub_n[tid] = 0u; s.sub_w[tid] = 0u; }
+    if (DT == FSD_F32)
+        for (int i = tid; i < 256; i += kRowThreads) { s.sub_n[i] = 0u; s.sub_w[i] = 0u; }
+    if (tid < 8) s.settings[tid] = setting;
     __syncthreads();
     cluster_arrive();                                       // from here on others may add to the first block's counts
     for (int j = tid; j < drafts; j += kRowThreads) {
@@ -864,7 +902,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_kernel(const ProcArgs 
             }
             row.vecs[i] = v;
             if (!cutting) continue;
-            tiny += count_vec<DT>(v, row.vecs + i, hist);
+            tiny += count_vec<DT>(v, hist);
             if constexpr (DT == FSD_F32) {
                 const uint32_t bits[4] = {v.x, v.y, v.z, v.w};
                 const uint32_t sparse = (history ? bits8(seen, t0, 4 * a.W) : 0u) | (drafts > 0 ? bits8(drafted_ids, t0 - word0 * 32, 4 * n_words) : 0u);
@@ -971,7 +1009,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_kernel(const ProcArgs 
             for (int k = 0; k < blocks; ++k) cluster.map_shared_rank(&s, tid)->top[k] = s.top[k];
     }
     int turn = 0;
-    CutResult res = tell_result(s, cluster, rank, blocks, turn);
+    CutResult res = tell_result(s, cluster, rank, blocks, turn, DT == FSD_F32);
     if constexpr (DT == FSD_F32) {
         if (res.kind == kCutRefineK || res.kind == kCutRefineP) {
             top = 0u;
@@ -1008,20 +1046,42 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_kernel(const ProcArgs 
     }
     const long long ties = res.kind == kCutDone ? res.ties : a.V;
     const float value = value_of<DT>(key);
-    // Where only the first `ties` of the tokens at the cut are kept, each warp has a run of the slice and counts those before it.
+    // Where only the first `ties` of the tokens at the cut are kept: how many of them are in front of this block's.  bf16: the other
+    // blocks' counts say it, the first block's own being what is missing from the sum, which it has.
+    long long before = 0;
+    bool count = ties < a.V;
+    if (DT == FSD_BF16 && count) {
+        const int bin = bin_of_value(value);
+        uint32_t mine = 0u, behind = 0u;
+        uint32_t theirs[kMaxCutCluster];
+#pragma unroll
+        for (int k = 1; k < kMaxCutCluster; ++k) theirs[k] = k < blocks && k >= rank ? *cluster.map_shared_rank(hist + bin, k) : 0u;
+#pragma unroll
+        for (int k = 1; k < kMaxCutCluster; ++k) {
+            behind += theirs[k];
+            if (k == rank) mine = theirs[k];
+        }
+        if (rank == 0) mine = res.equal - behind;
+        else before = static_cast<long long>(res.equal) - behind;
+        if (before >= ties || before + mine <= ties) count = false;
+        cluster_arrive();                                   // (none leaves before the others have read its counts)
+    }
+    // Each warp has a run of the slice, and counts those in it.
     const int run = (row.n + kRowWarps - 1) / kRowWarps, w0 = warp * run < row.n ? warp * run : row.n, w1 = w0 + run < row.n ? w0 + run : row.n;
-    int left = INT_MAX, mine = 0;                           // how many of those in the warp's run are kept, and how many there are
-    if (ties < a.V) {
+    int left = ties < a.V && before >= ties ? 0 : INT_MAX, mine = 0;      // how many of those in the warp's run are kept, and how many there are
+    if (count) {
         for (int i = w0 + lane; i < w1; i += 32) mine += equal_in<DT>(row.vecs[i], value);
         mine = __reduce_add_sync(0xffffffffu, mine);
-        if (lane == 0) s.warp_equal[warp] = mine;
+        if (lane == 0) s.warp_n[warp] = static_cast<uint32_t>(mine);
         __syncthreads();
         int sum = 0, ahead = 0;
-        for (int w = 0; w < kRowWarps; ++w) { if (w == warp) ahead = sum; sum += s.warp_equal[w]; }
-        if (tid < blocks) cluster.map_shared_rank(&s, tid)->equal[rank] = sum;
-        cluster_barrier();
-        long long before = ahead;
-        for (int k = 0; k < rank; ++k) before += s.equal[k];
+        for (int w = 0; w < kRowWarps; ++w) { if (w == warp) ahead = sum; sum += static_cast<int>(s.warp_n[w]); }
+        if constexpr (DT == FSD_F32) {
+            if (tid < blocks) cluster.map_shared_rank(&s, tid)->equal[rank] = sum;
+            cluster_barrier();
+            for (int k = 0; k < rank; ++k) before += s.equal[k];
+        }
+        before += ahead;
         left = ties <= before ? 0 : ties - before < mine ? static_cast<int>(ties - before) : INT_MAX;
     }
     const bool some = left > 0 && left != INT_MAX;          // the one run that the last of them is in
@@ -1051,6 +1111,264 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_kernel(const ProcArgs 
             v = cut_vec<DT>(v, value, above);
         }
         if (in_run) store_ids<DT>(out, t0, a.V, t0 >= 0 && t0 + N <= a.V && alike, v);
+    }
+    if (DT == FSD_BF16 && ties < a.V) cluster_wait();
+}
+
+// ---- bf16: a block per row ---------------------------------------------------------------
+// The block reads the row twice and keeps none of it: once to count its values, and again, from the L2 cache for the most part
+// (two blocks an SM have 90 MB of rows of 152064 on the way), to write it.  No block waits for another, which is what most of
+// a cluster's time went into: 64 x 17 x 152064 took 660 us that way.
+// Sparse ids, whose penalties the count leaves out at first, are listed in front: a bitmap of the row's, the sum of its bits up to each word, and for
+// each id what becomes of it, worked out once, one a thread, when what was counted for it is taken back.
+struct RowsShape {             // of the dynamic shared memory; the last two are in words and ids
+    int words, cap;
+};
+struct RowsShared {
+    CutShared cut;
+    uint32_t equal[2][kRowWarps];
+    int n_sparse;
+};
+
+__device__ __forceinline__ float value_at(const uint4& v, int e) {
+    const uint32_t w = e < 4 ? (e < 2 ? v.x : v.y) : (e < 6 ? v.z : v.w);
+    return (e & 1) ? bf16_hi(w) : bf16_lo(w);
+}
+__device__ __forceinline__ void put_at(uint4& v, int e, uint32_t half) {
+    const uint32_t sel = (e & 1) ? 0x5410u : 0x3254u;
+    const int w = e >> 1;
+    v.x = w == 0 ? __byte_perm(v.x, half, sel) : v.x;
+    v.y = w == 1 ? __byte_perm(v.y, half, sel) : v.y;
+    v.z = w == 2 ? __byte_perm(v.z, half, sel) : v.z;
+    v.w = w == 3 ? __byte_perm(v.w, half, sel) : v.w;
+}
+
+__global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const ProcArgs a, const RowsShape shape, bool raw) {
+    constexpr int DT = FSD_BF16, N = 8, kAtOnce = 4, kTile = kAtOnce * kRowThreads;
+    extern __shared__ uint4 on_chip[];
+    __shared__ RowsShared s;
+    uint32_t* hist = reinterpret_cast<uint32_t*>(on_chip);
+    uint32_t* bitmap = hist + kBins;                        // of the sparse ids
+    uint32_t* list = bitmap + shape.words;                  // them
+    uint16_t* becomes = reinterpret_cast<uint16_t*>(list + shape.cap);
+    uint16_t* ahead = becomes + shape.cap;                  // how many of them are in front of a word
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int all = a.rows[0] + a.rows[1], b = blockIdx.x / all, q = blockIdx.x % all;
+    const int side = q >= a.rows[0], r = q - (side ? a.rows[0] : 0);
+    const size_t at = (static_cast<size_t>(b) * a.rows[side] + r) * a.V;
+    const uint16_t* in = static_cast<const uint16_t*>(raw ? a.out[side] : a.in[side]) + at;
+    uint16_t* out = static_cast<uint16_t*>(a.out[side]) + at;
+    const int lies = static_cast<int>(reinterpret_cast<uintptr_t>(in) % 16 / 2);
+    const bool alike = (reinterpret_cast<uintptr_t>(in) ^ reinterpret_cast<uintptr_t>(out)) % 16 == 0;
+    const int n_vecs = (a.V + lies + N - 1) / N;
+    // a warp has kAtOnce runs of 32 vectors of a tile, one behind the other
+    const auto vec_of = [&](int tile, int u) { return tile + (warp * kAtOnce + u) * 32 + lane; };
+    uint4 got[kAtOnce];
+    const auto fetch = [&](int tile) {
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int i = vec_of(tile, u), t0 = i * N - lies;
+            if (i < n_vecs) got[u] = load_ids<DT>(in, t0, a.V, t0 >= 0 && t0 + N <= a.V);
+        }
+    };
+    uint32_t setting = 0u;
+    if (tid < 8) {                                          // the sequence's settings, all read at once
+        const void* const at_b[8] = {a.top_k, a.top_p, a.min_p, raw ? nullptr : a.repetition, raw ? nullptr : a.frequency, raw ? nullptr : a.presence,
+                                     raw ? nullptr : a.temperature, nullptr};
+        const void* from = nullptr;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) from = k == tid ? at_b[k] : from;
+        setting = from != nullptr ? __ldg(static_cast<const uint32_t*>(from) + b) : tid == 1 || tid == 3 ? 0x3f800000u : 0u;
+    }
+    fetch(0);
+    const int ctx = context_row(a, b, side, r);
+    const int drafts = !raw && a.penalties && a.tokens != nullptr && ctx > 0 ? a.P : 0;
+    const bool history = !raw && a.penalties && a.seen != nullptr, sparse = history || drafts > 0;
+    const uint32_t* seen = history ? a.seen + static_cast<size_t>(b) * a.W : nullptr;
+    const uint32_t* allowed = !raw && a.allowed != nullptr ? a.allowed + (static_cast<size_t>(b) * (a.P + 1) + ctx) * a.W : nullptr;
+    for (int i = tid; i < kBins / 4; i += kRowThreads) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (tid < 8) s.cut.settings[tid] = setting;
+    if (sparse) {
+        for (int w = tid; w < a.W; w += kRowThreads) {
+            uint32_t bits = history ? __ldg(seen + w) : 0u;
+            if (allowed != nullptr) bits &= __ldg(allowed + w);
+            if (w == a.W - 1 && (a.V & 31)) bits &= (1u << (a.V & 31)) - 1u;
+            bitmap[w] = bits;
+        }
+    }
+    __syncthreads();
+    const CutParams c = cut_params(s.cut.settings, a.V);
+    const SeqParams p = seq_params(s.cut.settings + 3);
+    const bool cutting = c.k || c.p || c.m;
+    const auto process = [&](const uint4& v, int t0) {
+        uint32_t may = allowed != nullptr ? bits8(allowed, t0, 4 * a.W) : 0xffu;
+        if (t0 < 0 || t0 + N > a.V) may &= ids_of<N>(t0, a.V);                // (what is not in the row counts as masked)
+        return process_vec<DT>(v, may, p.inv_temp);
+    };
+    // what becomes of a sparse id
+    const auto value_of_id = [&](int t, float x, int count) {
+        return process_id(x, count, drafts > 0 ? drafted(a, b, ctx, t) : 0, 0.f, false, p);
+    };
+    bool listed = false;
+    if (sparse) {
+        if (drafts > 0) {
+            for (int j = ctx - 1 - tid; j >= 0 && a.parent == nullptr; j -= kRowThreads) {
+                const int t = __ldg(a.tokens + static_cast<size_t>(b) * a.P + j);
+                if (t >= 0 && t < a.V && (allowed == nullptr || (__ldg(allowed + (t >> 5)) >> (t & 31) & 1u))) atomicOr(&bitmap[t >> 5], 1u << (t & 31));
+            }
+            if (a.parent != nullptr && tid == 0)
+                for (int j = ctx - 1; j >= 0; j = node_before(a, b, j)) {
+                    const int t = __ldg(a.tokens + static_cast<size_t>(b) * a.P + j);
+                    if (t >= 0 && t < a.V && (allowed == nullptr || (__ldg(allowed + (t >> 5)) >> (t & 31) & 1u))) atomicOr(&bitmap[t >> 5], 1u << (t & 31));
+                }
+            __syncthreads();
+        }
+        const int each = (a.W + kRowThreads - 1) / kRowThreads, w0 = tid * each, w1 = w0 + each < a.W ? w0 + each : a.W;
+        Run mine = {0u, 0.0}, total;
+        for (int w = w0; w < w1; ++w) mine.n += __popc(bitmap[w]);
+        uint32_t n = scan_threads(mine, s.cut, total).n;
+        listed = total.n <= static_cast<uint32_t>(shape.cap);                 // (else each vector works its own out)
+        if (tid == 0) s.n_sparse = static_cast<int>(total.n);
+        if (listed)
+            for (int w = w0; w < w1; ++w) {
+                ahead[w] = static_cast<uint16_t>(n);
+                for (uint32_t todo = bitmap[w]; todo != 0u; todo &= todo - 1u) list[n++] = w * 32 + __ffs(static_cast<int>(todo)) - 1;
+            }
+    }
+    __syncthreads();
+    const int n_sparse = sparse ? s.n_sparse : 0;
+    // a vector with its sparse ids as they become
+    const auto patch = [&](uint4 v, const uint4& was, int t0) {
+        uint32_t todo = bits8(bitmap, t0, 4 * a.W);
+        while (todo != 0u) {
+            const int e = __ffs(static_cast<int>(todo)) - 1, t = t0 + e;
+            todo &= todo - 1u;
+            uint32_t half;
+            if (listed) {
+                half = becomes[ahead[t >> 5] + __popc(bitmap[t >> 5] & ((1u << (t & 31)) - 1u))];
+            } else {
+                const bool used = history && (__ldg(seen + (t >> 5)) >> (t & 31) & 1u);
+                half = pack_bf16(value_of_id(t, value_at(was, e), used ? __ldg(a.counts + static_cast<size_t>(b) * a.V + t) : -1), 0.f);
+            }
+            put_at(v, e, half);
+        }
+        return v;
+    };
+
+    CutResult res = {kCutNone, 0u, a.V, 0u, 0u};
+    if (cutting) {
+        double tiny = 0.0;
+        for (int tile = 0; tile < n_vecs; tile += kTile) {
+            if (tile > 0) fetch(tile);
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                const int i = vec_of(tile, u), t0 = i * N - lies;
+                if (i >= n_vecs) break;
+                uint4 v = process(got[u], t0);
+                if (n_sparse > 0 && !listed) v = patch(v, got[u], t0);
+                tiny += count_vec<DT>(v, hist);
+            }
+        }
+        if (listed) {
+            const uint16_t* row = in;
+#pragma unroll 4
+            for (int k = tid; k < n_sparse; k += kRowThreads) {
+                const int t = list[k];
+                const bool used = history && (__ldg(seen + (t >> 5)) >> (t & 31) & 1u);
+                const int count = used ? __ldg(a.counts + static_cast<size_t>(b) * a.V + t) : -1;
+                const float x = read_id<DT>(row, t);
+                const uint32_t was = pack_bf16(__fmul_rn(x, p.inv_temp), 0.f) & 0xffffu, now = pack_bf16(value_of_id(t, x, count), 0.f) & 0xffffu;
+                becomes[k] = static_cast<uint16_t>(now);
+                tiny += count_value<1>(now << 16, hist) - count_value<-1>(was << 16, hist);
+            }
+        }
+        if (__any_sync(0xffffffffu, tiny != 0.0)) tiny = warp_sum(tiny);
+        if (lane == 0) s.cut.warp_w[warp] = tiny;
+        __syncthreads();
+        if (tid == 0) {
+            tiny = 0.0;
+#pragma unroll
+            for (int w = 0; w < kRowWarps; ++w) tiny += s.cut.warp_w[w];
+            s.cut.tiny[0] = tiny;
+        }
+        __syncthreads();
+        solve_bins<DT>(hist, s.cut, c, 1, a.V);
+        __syncthreads();
+        res = s.cut.work;
+    } else if (listed) {
+        for (int k = tid; k < n_sparse; k += kRowThreads) {
+            const int t = list[k];
+            const bool used = history && (__ldg(seen + (t >> 5)) >> (t & 31) & 1u);
+            becomes[k] = static_cast<uint16_t>(pack_bf16(value_of_id(t, read_id<DT>(in, t), used ? __ldg(a.counts + static_cast<size_t>(b) * a.V + t) : -1), 0.f));
+        }
+        __syncthreads();
+    }
+
+    // the row again, cut off
+    const bool cut = res.kind == kCutDone;
+    const float value = value_of<DT>(res.key);
+    long long left = cut && res.ties < a.V ? res.ties : LLONG_MAX;             // how many of the tokens equal to the cut are still kept
+    int turn = 0;
+    for (int tile = 0; tile < n_vecs; tile += kTile) {
+        if (tile > 0 || n_vecs > kTile || !cutting) fetch(tile);
+        int equal = 0;
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int i = vec_of(tile, u), t0 = i * N - lies;
+            if (i >= n_vecs) break;
+            uint4 v = process(got[u], t0);
+            if (n_sparse > 0) v = patch(v, got[u], t0);
+            got[u] = v;
+            if (left > 0 && left != LLONG_MAX) equal += equal_in<DT>(v, value);
+        }
+        int mine = INT_MAX;                                 // what of them is left for the warp's vectors
+        if (left > 0 && left != LLONG_MAX) {
+            equal = __reduce_add_sync(0xffffffffu, equal);
+            turn ^= 1;
+            if (lane == 0) s.equal[turn][warp] = static_cast<uint32_t>(equal);
+            __syncthreads();
+            int before = 0, sum = 0;
+#pragma unroll
+            for (int w = 0; w < kRowWarps; ++w) {
+                if (w == warp) before = sum;
+                sum += static_cast<int>(s.equal[turn][w]);
+            }
+            mine = left <= before ? 0 : left - before < equal ? static_cast<int>(left - before) : INT_MAX;
+            left = left > sum ? left - sum : 0;
+        } else if (left == 0) {
+            mine = 0;
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int i = vec_of(tile, u), t0 = i * N - lies;
+            uint4 v = got[u];
+            if (cut) {
+                if (mine > 0 && mine != INT_MAX) {          // the one warp that the last of them is in
+                    const int n = i < n_vecs ? equal_in<DT>(v, value) : 0;
+                    int sum = n;
+#pragma unroll
+                    for (int d = 1; d < 32; d <<= 1) {
+                        const int o = __shfl_up_sync(0xffffffffu, sum, d);
+                        if (lane >= d) sum += o;
+                    }
+                    v = cut_some<DT>(v, value, mine - (sum - n), N);
+                    mine -= __shfl_sync(0xffffffffu, sum, 31);
+                    mine = mine > 0 ? mine : 0;
+                } else {
+                    v = cut_vec<DT>(v, value, mine == 0);
+                }
+            }
+            if (i < n_vecs) store_ids<DT>(out, t0, a.V, t0 >= 0 && t0 + N <= a.V && alike, v);
+        }
+    }
+    if (res.kind != kCutByBits) return;
+    __syncthreads();                                        // (what the block stored is seen by all of it)
+    const Cut by_bits = find_cut<DT>(out, a.V, 0, a.V, c, [&](CountAndWeight v) { return block_total(v, s.cut.scratch); },
+                                     [&](uint32_t k) { return block_largest(k, s.cut.scratch); });
+    if (!by_bits.any) return;
+    for (int i = tid; i < a.V; i += kRowThreads) {
+        const uint32_t k = key_of<DT>(out[i]);
+        if (k < by_bits.key || (k == by_bits.key && i >= by_bits.until)) out[i] = 0xff80u;
     }
 }
 
