@@ -10,6 +10,8 @@
 #include "fsd_history.cuh"
 #include "fsd_process.cuh"
 #include "fsd_truncate.cuh"
+#include "fsd_truncate_cluster.cuh"
+#include "fsd_truncate_rows.cuh"
 
 namespace {
 
@@ -43,15 +45,14 @@ int check(const fsd_process_opts* o) {
     return FSD_OK;
 }
 
-// How a row lies in the shared memory of a cluster's blocks.
+// fp32: how a row lies in the shared memory of a cluster's blocks.
 struct CutShape {
     int blocks, slice;         // slice: vectors a block has
     size_t smem;
     bool fits;
 };
-template <int DT>
 CutShape cut_shape(const ProcArgs& a, bool raw) {
-    constexpr int N = Logit<DT>::kPerVec;
+    constexpr int N = Logit<FSD_F32>::kPerVec;
     CutShape c;
     const long long rows = static_cast<long long>(a.B) * (a.rows[0] + a.rows[1]);
     const int vecs = (a.V + 2 * (N - 1)) / N;             // a row's, wherever it starts
@@ -64,68 +65,73 @@ CutShape cut_shape(const ProcArgs& a, bool raw) {
     return c;
 }
 
-// bf16: whether a block does a row by itself, and its shared memory: the bins, and where there are sparse ids their bitmap and list, of 8192
-// of them if two blocks an SM have room for it.
+// bf16: the shared memory of a block that does a row: the bins, and where there are sparse ids their bitmap and list, of 8192 of them if
+// two blocks an SM have room for it.  False where the vocabulary is too long for that.
 bool rows_shape(const ProcArgs& a, bool raw, RowsShape* shape, size_t* smem) {
+    constexpr long long kTwo = 110 * 1024;                // what two blocks an SM may have each
     const bool sparse = !raw && a.penalties && (a.seen != nullptr || a.tokens != nullptr);
     shape->words = sparse ? (a.W + 3) / 4 * 4 : 0;
     shape->cap = 0;
-    const size_t fixed = kBins * sizeof(uint32_t) + static_cast<size_t>(shape->words) * 6;
+    const long long fixed = static_cast<long long>(kBins) * 4 + static_cast<long long>(shape->words) * 6;
     if (sparse) {
-        const long long room = (fixed < 90 * 1024 ? 94 * 1024ll : 190 * 1024ll) - static_cast<long long>(fixed);
+        const long long room = (fixed + 6 * 2048 <= kTwo ? kTwo : static_cast<long long>(kCutSmem)) - fixed;
         if (room < 6 * 256) return false;
         shape->cap = static_cast<int>(room / 6 < 8192 ? room / 6 / 8 * 8 : 8192);
     }
-    *smem = fixed + static_cast<size_t>(shape->cap) * 6;
+    *smem = static_cast<size_t>(fixed) + static_cast<size_t>(shape->cap) * 6;
     return true;
 }
 
-// Rows that are cut off: a cluster of blocks holds a row in shared memory where it fits, else a block sweeps over it in memory.
-template <int DT>
-int launch_cut(const ProcArgs& a, bool raw, cudaStream_t s) {
+// Once a device: the kernels' attributes, and the table they read.
+int prepare_cut() {
     constexpr int kDevices = 64;
     static bool ready[kDevices] = {};
+    static double weights[kBins];
     static std::mutex mu;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices) return FSD_ERR_CUDA;
-    {
-        std::lock_guard<std::mutex> lock(mu);
-        if (!ready[dev]) {
-            if (cudaFuncSetAttribute(fsd_cut_kernel<DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kCutSmem)) != cudaSuccess) return FSD_ERR_CUDA;
-            if (DT == FSD_BF16 && cudaFuncSetAttribute(fsd_cut_rows_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kCutSmem)) != cudaSuccess)
-                return FSD_ERR_CUDA;
-            static double weights[kBins];                 // (under the lock)
-            fill_bin_weights(weights);
-            if (cudaMemcpyToSymbol(bin_weights, weights, sizeof weights) != cudaSuccess) return FSD_ERR_CUDA;
-            ready[dev] = true;
-        }
-    }
+    std::lock_guard<std::mutex> lock(mu);
+    if (ready[dev]) return FSD_OK;
+    if (cudaFuncSetAttribute(fsd_cut_cluster_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kCutSmem)) != cudaSuccess ||
+        cudaFuncSetAttribute(fsd_cut_rows_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kCutSmem)) != cudaSuccess)
+        return FSD_ERR_CUDA;
+    fill_bin_weights(weights);
+    if (cudaMemcpyToSymbol(bin_weights, weights, sizeof weights) != cudaSuccess) return FSD_ERR_CUDA;
+    ready[dev] = true;
+    return FSD_OK;
+}
+
+// Rows that are cut off.  fp32: a cluster of blocks holds a row in shared memory where it fits, else a block sweeps over it in memory.
+template <int DT>
+int launch_cut(const ProcArgs& a, bool raw, cudaStream_t s) {
+    const int rc = prepare_cut();
+    if (rc != FSD_OK) return rc;
+    const long long rows = static_cast<long long>(a.B) * (a.rows[0] + a.rows[1]);
     if constexpr (DT == FSD_BF16) {
         RowsShape shape;
         size_t smem;
-        if (rows_shape(a, raw, &shape, &smem)) {
-            fsd_cut_rows_kernel<<<static_cast<unsigned>(a.B) * (a.rows[0] + a.rows[1]), kRowThreads, smem, s>>>(a, shape, raw);
+        if (!rows_shape(a, raw, &shape, &smem)) return FSD_ERR_SHAPE;
+        fsd_cut_rows_kernel<<<static_cast<unsigned>(rows), kRowThreads, smem, s>>>(a, shape, raw);
+        return cudaGetLastError() == cudaSuccess ? FSD_OK : FSD_ERR_CUDA;
+    } else {
+        const CutShape c = cut_shape(a, raw);
+        if (rows * c.blocks > INT_MAX) return FSD_ERR_SHAPE;
+        if (!c.fits) {
+            fsd_cut_long_kernel<DT><<<static_cast<unsigned>(rows), kLongThreads, 0, s>>>(a);
             return cudaGetLastError() == cudaSuccess ? FSD_OK : FSD_ERR_CUDA;
         }
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(static_cast<unsigned>(rows * c.blocks), 1, 1);
+        cfg.blockDim = dim3(kRowThreads, 1, 1);
+        cfg.dynamicSmemBytes = c.smem;
+        cfg.stream = s;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = static_cast<unsigned>(c.blocks); attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        return cudaLaunchKernelEx(&cfg, fsd_cut_cluster_kernel, a, c.slice, raw) == cudaSuccess ? FSD_OK : FSD_ERR_CUDA;
     }
-    const CutShape c = cut_shape<DT>(a, raw);
-    const long long rows = static_cast<long long>(a.B) * (a.rows[0] + a.rows[1]);
-    if (rows * c.blocks > INT_MAX) return FSD_ERR_SHAPE;
-    if (!c.fits) {
-        fsd_cut_long_kernel<DT><<<static_cast<unsigned>(rows), kLongThreads, 0, s>>>(a);
-        return cudaGetLastError() == cudaSuccess ? FSD_OK : FSD_ERR_CUDA;
-    }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(rows * c.blocks), 1, 1);
-    cfg.blockDim = dim3(kRowThreads, 1, 1);
-    cfg.dynamicSmemBytes = c.smem;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = static_cast<unsigned>(c.blocks); attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, fsd_cut_kernel<DT>, a, c.slice, raw) == cudaSuccess ? FSD_OK : FSD_ERR_CUDA;
 }
 
 template <int DT>
@@ -134,7 +140,7 @@ int launch(const ProcArgs& a, bool cut, cudaStream_t s) {
     // The cut kernel does the rest too where it has room for it and there are no biases (whose lookup wants room there).
     RowsShape shape;
     size_t smem;
-    const bool room = DT == FSD_BF16 ? rows_shape(a, false, &shape, &smem) : cut_shape<DT>(a, false).fits;
+    const bool room = DT == FSD_BF16 ? rows_shape(a, false, &shape, &smem) : cut_shape(a, false).fits;
     if (cut && a.bias_offsets == nullptr && room) return launch_cut<DT>(a, false, s);
     // a row's vectors, wherever it starts, by blocks
     const long long spans = (a.V + 2 * (Logit<DT>::kPerVec - 1)) / Logit<DT>::kPerVec / kProcThreads + 1;

@@ -1,0 +1,255 @@
+// Top-k, top-p and min-p on rows of bf16 logits: a block per row.
+#pragma once
+
+#include "fsd_truncate.cuh"
+
+namespace fsd {
+
+// The block reads the row twice and keeps none of it: once to count its values, and again, from the L2 cache for the most part
+// (two blocks an SM have 90 MB of rows of 152064 on the way), to write it.  No block waits for another, which is what most of
+// a cluster's time went into: 64 x 17 x 152064 took 660 us that way.
+// Sparse ids, whose penalties the count leaves out at first, are listed in front: a bitmap of the row's, the sum of its bits up to each word, and for
+// each id what becomes of it, worked out once, one a thread, when what was counted for it is taken back.
+struct RowsShape {             // of the dynamic shared memory; the last two are in words and ids
+    int words, cap;
+};
+struct RowsShared {
+    BinsShared cut;
+    uint32_t equal[2][kRowWarps];
+    int n_sparse;
+};
+
+__device__ __forceinline__ float value_at(const uint4& v, int e) {
+    const uint32_t w = e < 4 ? (e < 2 ? v.x : v.y) : (e < 6 ? v.z : v.w);
+    return (e & 1) ? bf16_hi(w) : bf16_lo(w);
+}
+__device__ __forceinline__ void put_at(uint4& v, int e, uint32_t half) {
+    const uint32_t sel = (e & 1) ? 0x5410u : 0x3254u;
+    const int w = e >> 1;
+    v.x = w == 0 ? __byte_perm(v.x, half, sel) : v.x;
+    v.y = w == 1 ? __byte_perm(v.y, half, sel) : v.y;
+    v.z = w == 2 ? __byte_perm(v.z, half, sel) : v.z;
+    v.w = w == 3 ? __byte_perm(v.w, half, sel) : v.w;
+}
+
+__global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const ProcArgs a, const RowsShape shape, bool raw) {
+    constexpr int DT = FSD_BF16, N = 8, kAtOnce = 4, kTile = kAtOnce * kRowThreads;
+    extern __shared__ uint4 on_chip[];
+    __shared__ RowsShared s;
+    uint32_t* hist = reinterpret_cast<uint32_t*>(on_chip);
+    uint32_t* bitmap = hist + kBins;                        // of the sparse ids
+    uint32_t* list = bitmap + shape.words;                  // them
+    uint16_t* becomes = reinterpret_cast<uint16_t*>(list + shape.cap);
+    uint16_t* ahead = becomes + shape.cap;                  // how many of them are in front of a word
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int all = a.rows[0] + a.rows[1], b = blockIdx.x / all, q = blockIdx.x % all;
+    const int side = q >= a.rows[0], r = q - (side ? a.rows[0] : 0);
+    const size_t at = (static_cast<size_t>(b) * a.rows[side] + r) * a.V;
+    const uint16_t* in = static_cast<const uint16_t*>(raw ? a.out[side] : a.in[side]) + at;
+    uint16_t* out = static_cast<uint16_t*>(a.out[side]) + at;
+    const int lies = static_cast<int>(reinterpret_cast<uintptr_t>(in) % 16 / 2);
+    const bool alike = (reinterpret_cast<uintptr_t>(in) ^ reinterpret_cast<uintptr_t>(out)) % 16 == 0;
+    const int n_vecs = (a.V + lies + N - 1) / N;
+    // a warp has kAtOnce runs of 32 vectors of a tile, one behind the other
+    const auto vec_of = [&](int tile, int u) { return tile + (warp * kAtOnce + u) * 32 + lane; };
+    uint4 got[kAtOnce];
+    const auto fetch = [&](int tile) {
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int i = vec_of(tile, u), t0 = i * N - lies;
+            if (i < n_vecs) got[u] = load_ids<DT>(in, t0, a.V, t0 >= 0 && t0 + N <= a.V);
+        }
+    };
+    uint32_t setting = 0u;
+    if (tid < 8) {                                          // the sequence's settings, all read at once
+        const void* const at_b[8] = {a.top_k, a.top_p, a.min_p, raw ? nullptr : a.repetition, raw ? nullptr : a.frequency, raw ? nullptr : a.presence,
+                                     raw ? nullptr : a.temperature, nullptr};
+        const void* from = nullptr;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) from = k == tid ? at_b[k] : from;
+        setting = from != nullptr ? __ldg(static_cast<const uint32_t*>(from) + b) : tid == 1 || tid == 3 ? 0x3f800000u : 0u;
+    }
+    fetch(0);
+    const int ctx = context_row(a, b, side, r);
+    const int drafts = !raw && a.penalties && a.tokens != nullptr && ctx > 0 ? a.P : 0;
+    const bool history = !raw && a.penalties && a.seen != nullptr, sparse = history || drafts > 0;
+    const uint32_t* seen = history ? a.seen + static_cast<size_t>(b) * a.W : nullptr;
+    const uint32_t* allowed = !raw && a.allowed != nullptr ? a.allowed + (static_cast<size_t>(b) * (a.P + 1) + ctx) * a.W : nullptr;
+    clear_bins(hist, s.cut);
+    if (tid < 8) s.cut.settings[tid] = setting;
+    if (sparse) {
+        for (int w = tid; w < a.W; w += kRowThreads) {
+            uint32_t bits = history ? __ldg(seen + w) : 0u;
+            if (allowed != nullptr) bits &= __ldg(allowed + w);
+            if (w == a.W - 1 && (a.V & 31)) bits &= (1u << (a.V & 31)) - 1u;
+            bitmap[w] = bits;
+        }
+    }
+    __syncthreads();
+    const CutParams c = cut_params(s.cut.settings, a.V);
+    const SeqParams p = seq_params(s.cut.settings + 3);
+    const bool cutting = c.k || c.p || c.m;
+    const auto process = [&](const uint4& v, int t0) {
+        uint32_t may = allowed != nullptr ? bits8(allowed, t0, 4 * a.W) : 0xffu;
+        if (t0 < 0 || t0 + N > a.V) may &= ids_of<N>(t0, a.V);                // (what is not in the row counts as masked)
+        return process_vec<DT>(v, may, p.inv_temp);
+    };
+    // what becomes of a sparse id
+    const auto value_of_id = [&](int t, float x, int count) {
+        return process_id(x, count, drafts > 0 ? drafted(a, b, ctx, t) : 0, 0.f, false, p);
+    };
+    bool listed = false;
+    if (sparse) {
+        if (drafts > 0) {
+            for (int j = ctx - 1 - tid; j >= 0 && a.parent == nullptr; j -= kRowThreads) {
+                const int t = __ldg(a.tokens + static_cast<size_t>(b) * a.P + j);
+                if (t >= 0 && t < a.V && (allowed == nullptr || (__ldg(allowed + (t >> 5)) >> (t & 31) & 1u))) atomicOr(&bitmap[t >> 5], 1u << (t & 31));
+            }
+            if (a.parent != nullptr && tid == 0)
+                for (int j = ctx - 1; j >= 0; j = node_before(a, b, j)) {
+                    const int t = __ldg(a.tokens + static_cast<size_t>(b) * a.P + j);
+                    if (t >= 0 && t < a.V && (allowed == nullptr || (__ldg(allowed + (t >> 5)) >> (t & 31) & 1u))) atomicOr(&bitmap[t >> 5], 1u << (t & 31));
+                }
+            __syncthreads();
+        }
+        const int each = (a.W + kRowThreads - 1) / kRowThreads, w0 = tid * each, w1 = w0 + each < a.W ? w0 + each : a.W;
+        Run mine = {0u, 0.0}, total;
+        for (int w = w0; w < w1; ++w) mine.n += __popc(bitmap[w]);
+        uint32_t n = scan_threads(mine, s.cut, total).n;
+        listed = total.n <= static_cast<uint32_t>(shape.cap);                 // (else each vector works its own out)
+        if (tid == 0) s.n_sparse = static_cast<int>(total.n);
+        if (listed)
+            for (int w = w0; w < w1; ++w) {
+                ahead[w] = static_cast<uint16_t>(n);
+                for (uint32_t todo = bitmap[w]; todo != 0u; todo &= todo - 1u) list[n++] = w * 32 + __ffs(static_cast<int>(todo)) - 1;
+            }
+    }
+    __syncthreads();
+    const int n_sparse = sparse ? s.n_sparse : 0;
+    // a vector with its sparse ids as they become
+    const auto patch = [&](uint4 v, const uint4& was, int t0) {
+        uint32_t todo = bits8(bitmap, t0, 4 * a.W);
+        while (todo != 0u) {
+            const int e = __ffs(static_cast<int>(todo)) - 1, t = t0 + e;
+            todo &= todo - 1u;
+            uint32_t half;
+            if (listed) {
+                half = becomes[ahead[t >> 5] + __popc(bitmap[t >> 5] & ((1u << (t & 31)) - 1u))];
+            } else {
+                const bool used = history && (__ldg(seen + (t >> 5)) >> (t & 31) & 1u);
+                half = pack_bf16(value_of_id(t, value_at(was, e), used ? __ldg(a.counts + static_cast<size_t>(b) * a.V + t) : -1), 0.f);
+            }
+            put_at(v, e, half);
+        }
+        return v;
+    };
+
+    CutResult res = {kCutNone, 0u, a.V, 0u};
+    if (cutting) {
+        for (int tile = 0; tile < n_vecs; tile += kTile) {
+            if (tile > 0) fetch(tile);
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                const int i = vec_of(tile, u), t0 = i * N - lies;
+                if (i >= n_vecs) break;
+                uint4 v = process(got[u], t0);
+                if (n_sparse > 0 && !listed) v = patch(v, got[u], t0);
+                count_vec<DT>(v, hist, &s.cut);
+            }
+        }
+        if (listed) {
+            const uint16_t* row = in;
+#pragma unroll 4
+            for (int k = tid; k < n_sparse; k += kRowThreads) {
+                const int t = list[k];
+                const bool used = history && (__ldg(seen + (t >> 5)) >> (t & 31) & 1u);
+                const int count = used ? __ldg(a.counts + static_cast<size_t>(b) * a.V + t) : -1;
+                const float x = read_id<DT>(row, t);
+                const uint32_t was = pack_bf16(__fmul_rn(x, p.inv_temp), 0.f) & 0xffffu, now = pack_bf16(value_of_id(t, x, count), 0.f) & 0xffffu;
+                becomes[k] = static_cast<uint16_t>(now);
+                count_value<DT, 1>(now << 16, hist, &s.cut);
+                count_value<DT, -1>(was << 16, hist, &s.cut);
+            }
+        }
+        __syncthreads();
+        solve_bins<DT>(hist, s.cut, c, a.V, 0u);
+        __syncthreads();
+        res = s.cut.work;
+    } else if (listed) {
+        for (int k = tid; k < n_sparse; k += kRowThreads) {
+            const int t = list[k];
+            const bool used = history && (__ldg(seen + (t >> 5)) >> (t & 31) & 1u);
+            becomes[k] = static_cast<uint16_t>(pack_bf16(value_of_id(t, read_id<DT>(in, t), used ? __ldg(a.counts + static_cast<size_t>(b) * a.V + t) : -1), 0.f));
+        }
+        __syncthreads();
+    }
+
+    // the row again, cut off
+    const bool cut = res.kind == kCutDone;
+    const float value = value_of<DT>(res.key);
+    long long left = cut && res.ties < a.V ? res.ties : LLONG_MAX;             // how many of the tokens equal to the cut are still kept
+    int turn = 0;
+    for (int tile = 0; tile < n_vecs; tile += kTile) {
+        if (tile > 0 || n_vecs > kTile || !cutting) fetch(tile);
+        int equal = 0;
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int i = vec_of(tile, u), t0 = i * N - lies;
+            if (i >= n_vecs) break;
+            uint4 v = process(got[u], t0);
+            if (n_sparse > 0) v = patch(v, got[u], t0);
+            got[u] = v;
+            if (left > 0 && left != LLONG_MAX) equal += equal_in<DT>(v, value);
+        }
+        int mine = INT_MAX;                                 // what of them is left for the warp's vectors
+        if (left > 0 && left != LLONG_MAX) {
+            equal = __reduce_add_sync(0xffffffffu, equal);
+            turn ^= 1;
+            if (lane == 0) s.equal[turn][warp] = static_cast<uint32_t>(equal);
+            __syncthreads();
+            int before = 0, sum = 0;
+#pragma unroll
+            for (int w = 0; w < kRowWarps; ++w) {
+                if (w == warp) before = sum;
+                sum += static_cast<int>(s.equal[turn][w]);
+            }
+            mine = left <= before ? 0 : left - before < equal ? static_cast<int>(left - before) : INT_MAX;
+            left = left > sum ? left - sum : 0;
+        } else if (left == 0) {
+            mine = 0;
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int i = vec_of(tile, u), t0 = i * N - lies;
+            uint4 v = got[u];
+            if (cut) {
+                if (mine > 0 && mine != INT_MAX) {          // the one warp that the last of them is in
+                    const int n = i < n_vecs ? equal_in<DT>(v, value) : 0;
+                    int sum = n;
+#pragma unroll
+                    for (int d = 1; d < 32; d <<= 1) {
+                        const int o = __shfl_up_sync(0xffffffffu, sum, d);
+                        if (lane >= d) sum += o;
+                    }
+                    v = cut_some<DT>(v, value, mine - (sum - n), N);
+                    mine -= __shfl_sync(0xffffffffu, sum, 31);
+                    mine = mine > 0 ? mine : 0;
+                } else {
+                    v = cut_vec<DT>(v, value, mine == 0);
+                }
+            }
+            if (i < n_vecs) store_ids<DT>(out, t0, a.V, t0 >= 0 && t0 + N <= a.V && alike, v);
+        }
+    }
+    if (res.kind != kCutByBits) return;
+    __syncthreads();                                        // (what the block stored is seen by all of it)
+    const Cut by_bits = find_cut<DT>(out, a.V, 0, a.V, c, [&](CountAndWeight v) { return block_total(v, s.cut.scratch); },
+                                     [&](uint32_t k) { return block_largest(k, s.cut.scratch); });
+    if (!by_bits.any) return;
+    for (int i = tid; i < a.V; i += kRowThreads) {
+        const uint32_t k = key_of<DT>(out[i]);
+        if (k < by_bits.key || (k == by_bits.key && i >= by_bits.until)) out[i] = 0xff80u;
+    }
+}
+
+}  // namespace fsd
