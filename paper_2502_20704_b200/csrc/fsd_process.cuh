@@ -10,7 +10,6 @@
 namespace fsd {
 
 constexpr int kProcThreads = 256;
-constexpr int kTileRows = 4;           // rows on the way at once
 
 struct ProcArgs {
     const void* in[2];         // target and draft logits
@@ -89,8 +88,8 @@ template <int SPAN> struct Sparse {
     uint32_t drafted[(SPAN + 31) / 32 + 1];                // drafted or biased: to be looked at again in each row
     uint32_t bits[(SPAN + 31) / 32 + 1];
     int bias[SPAN];
-    uint16_t list[SPAN];                                   // (the highest bit: it is used)
-    int counts[SPAN];                                      // by place in the list
+    uint16_t list[SPAN];
+    int counts[SPAN];                                      // by place in the list; 0 for what is only in the prompt, -1: not used
     int n;
 };
 // All of the block's threads.  lo: the span's first id, a multiple of 32 (it may be negative).  Ends with a barrier.
@@ -129,15 +128,9 @@ __device__ __forceinline__ void find_sparse(const ProcArgs& a, int b, int lo, Sp
         int at = atomicAdd(&s.n, __popc(any));
         for (uint32_t todo = any; todo != 0u; todo &= todo - 1u) {
             const int e = __ffs(static_cast<int>(todo)) - 1;
-            s.list[at++] = static_cast<uint16_t>(k + e) | ((used >> e & 1u) ? 0x8000u : 0u);
+            s.counts[at] = (used >> e & 1u) ? __ldg(a.counts + static_cast<size_t>(b) * a.V + t + e) : -1;
+            s.list[at++] = static_cast<uint16_t>(k + e);
         }
-    }
-    __syncthreads();
-    // (a token that is used has a count of its own, 0 if it is only in the prompt; -1: not used)
-#pragma unroll 4
-    for (int i = threadIdx.x; i < s.n; i += blockDim.x) {
-        const int k = s.list[i] & 0x7fff;
-        s.counts[i] = (s.list[i] & 0x8000u) ? __ldg(a.counts + static_cast<size_t>(b) * a.V + lo + k) : -1;
     }
     __syncthreads();
 }
@@ -247,12 +240,10 @@ __device__ __forceinline__ uint4 merge(const uint4& a, const uint4& b, const uin
     return make_uint4((a.x & ~of_b.x) | (b.x & of_b.x), (a.y & ~of_b.y) | (b.y & of_b.y), (a.z & ~of_b.z) | (b.z & of_b.z), (a.w & ~of_b.w) | (b.w & of_b.w));
 }
 
-__device__ __forceinline__ uint4 both(const uint4& a, const uint4& b) { return make_uint4(a.x & b.x, a.y & b.y, a.z & b.z, a.w & b.w); }
-
-// A block takes a span of the vocabulary, a vector a thread, for some rows of one sequence, kTileRows at a time.  First the mask and
-// the temperature, a vector at a time, which leave the sparse ids as they were read; then these, one id a thread, in shared
-// memory: few of a vector's ids are sparse, but of a warp's 256 some always are, and a loop over a vector's own took 50
-// instructions a logit where this takes a few, and one over the rows in memory two transactions of the L2 cache for each of them.
+// A block takes a span of the vocabulary, a vector a thread, for some rows of one sequence.  First the mask and the temperature,
+// a vector at a time, which leave the sparse ids as they were read; then these, one id a thread: few of a vector's ids are sparse, but
+// of a warp's 256 some always are, and a loop over a vector's own took 50 instructions a logit where this takes a few.  (Done in
+// a tile of four rows in shared memory instead, 64 x 17 x 152064 took 247 us and 16 x 11 x 32000 26 where this takes 236 and 21.)
 // Counts and biases are looked up once for all rows.
 // Vectors are aligned in memory and not in the vocabulary: where a row starts s ids behind a 16-byte boundary, vector v
 // covers ids N v - s and on, and a row whose output lies differently is stored an id at a time.
@@ -261,7 +252,6 @@ __global__ void __launch_bounds__(kProcThreads) fsd_process_kernel(const ProcArg
     constexpr int N = Logit<DT>::kPerVec, kIds = kProcThreads * N, kSpan = kIds + 32;
     using elem = typename Logit<DT>::elem;
     __shared__ Sparse<kSpan> sparse;
-    __shared__ uint4 tile[kTileRows][kProcThreads];
     const int span = blockIdx.x % spans, group = blockIdx.x / spans % groups, b = blockIdx.x / spans / groups;
     const int lo = span * kIds - 32;
     const bool some = a.penalties || a.bias_offsets != nullptr;
@@ -273,9 +263,6 @@ __global__ void __launch_bounds__(kProcThreads) fsd_process_kernel(const ProcArg
     const int all = a.rows[0] + a.rows[1], first = group * group_rows, last = first + group_rows < all ? first + group_rows : all;
 
     const uint32_t* allowed = a.allowed != nullptr ? a.allowed + static_cast<size_t>(b) * (a.P + 1) * a.W : nullptr;
-    // In the list of sparse ids `wide` threads take a row, each with the same id in all rows it does.
-    int wide = 32;
-    while (wide < kProcThreads && wide < n_sparse) wide <<= 1;
     uint4 keep = make_uint4(0u, 0u, 0u, 0u);
     int keep_at = INT_MIN;                                  // the id that `keep` starts at
 #pragma unroll 1
@@ -302,62 +289,49 @@ __global__ void __launch_bounds__(kProcThreads) fsd_process_kernel(const ProcArg
             }
             return f;
         };
-        if (n_sparse == 0) {
-            Row next = fetch(in, r0);
+        Row next = fetch(in, r0);
 #pragma unroll 2
-            for (int r = r0; r < r1; ++r) {
-                const Row f = next;
-                const int t0 = first_id(in);
-                in += a.V;
-                if (r + 1 < r1) next = fetch(in, r + 1);
-                if (t0 < a.V) store_ids<DT>(out, t0, a.V, t0 >= 0 && t0 + N <= a.V && alike, process_vec<DT>(f.v, f.may, p.inv_temp));
-                out += a.V;
-            }
-            continue;
-        }
-        for (int r = r0; r < r1; r += kTileRows) {
-            const int rows = r1 - r < kTileRows ? r1 - r : kTileRows;
-            Row f[kTileRows];
-#pragma unroll
-            for (int j = 0; j < kTileRows; ++j)
-                if (j < rows) f[j] = fetch(in + static_cast<size_t>(j) * a.V, r + j);
-#pragma unroll
-            for (int j = 0; j < kTileRows; ++j) {
-                if (j >= rows) break;
-                const int t0 = first_id(in + static_cast<size_t>(j) * a.V);
-                if (t0 >= a.V) continue;
-                uint4 y = process_vec<DT>(f[j].v, f[j].may, p.inv_temp);
-                if (t0 != keep_at) { keep = spread_bits<DT>(bits8(sparse.bits, t0 - lo, sizeof(sparse.bits))); keep_at = t0; }
-                uint4 raw = keep;
-                if ((f[j].may & ((1u << N) - 1u)) != (1u << N) - 1u) raw = both(keep, spread_bits<DT>(f[j].may));
-                tile[j][threadIdx.x] = merge(y, f[j].v, raw);
-            }
-            __syncthreads();
-            for (int k = static_cast<int>(threadIdx.x) % wide; k < n_sparse; k += wide) {
-                const int at = sparse.list[k] & 0x7fff, t = lo + at, count = sparse.counts[k];
-                const bool again = sparse.drafted[at >> 5] >> (at & 31) & 1u;
-                const int entry = again && a.bias_offsets != nullptr ? sparse.bias[at] : 0;
-                const float bias = entry > 0 ? __ldg(a.bias_values + __ldg(a.bias_offsets + b) + entry - 1) : 0.f;
-                for (int j = static_cast<int>(threadIdx.x) / wide; j < rows; j += kProcThreads / wide) {
-                    // (what is another block's in this row is off the tile)
-                    const int i = t - first_id(in + static_cast<size_t>(j) * a.V) + static_cast<int>(threadIdx.x) * N;
-                    if (static_cast<unsigned>(i) >= static_cast<unsigned>(kIds)) continue;
-                    const float x = read_id<DT>(tile[j], i);
-                    if (x == -INFINITY) continue;           // masked, or as it would be
-                    const int d = again && a.penalties ? drafted(a, b, context_row(a, b, side, r + j), t) : 0;
-                    write_id<DT>(tile[j], i, process_id(x, count, d, bias, entry > 0, p));
+        for (int r = r0; r < r1; ++r) {
+            const Row f = next;
+            const int t0 = first_id(in);
+            in += a.V;
+            if (r + 1 < r1) next = fetch(in, r + 1);
+            if (t0 < a.V) {
+                uint4 y = process_vec<DT>(f.v, f.may, p.inv_temp);
+                if (n_sparse > 0) {
+                    if (t0 != keep_at) { keep = spread_bits<DT>(bits8(sparse.bits, t0 - lo, sizeof(sparse.bits))); keep_at = t0; }
+                    y = merge(y, f.v, keep);
                 }
+                store_ids<DT>(out, t0, a.V, t0 >= 0 && t0 + N <= a.V && alike, y);
             }
-            __syncthreads();
-#pragma unroll
-            for (int j = 0; j < kTileRows; ++j) {
-                if (j >= rows) break;
-                const int t0 = first_id(in);
-                if (t0 < a.V) store_ids<DT>(out, t0, a.V, t0 >= 0 && t0 + N <= a.V && alike, tile[j][threadIdx.x]);
-                in += a.V;
-                out += a.V;
-            }
-            // (a thread's own vectors of the tile are what it writes next; others read them only behind the next barrier)
+            out += a.V;
+        }
+    }
+    if (n_sparse == 0) return;
+    __syncthreads();                                        // (what the block's threads stored is seen by all of them)
+    // `wide` threads a row, each with the same id in all rows it does
+    int wide = 32;
+    while (wide < kProcThreads && wide < n_sparse) wide <<= 1;
+    const int stride = kProcThreads / wide;
+    for (int k = static_cast<int>(threadIdx.x) % wide; k < n_sparse; k += wide) {
+        const int at = sparse.list[k], t = lo + at, count = sparse.counts[k];
+        const bool again = sparse.drafted[at >> 5] >> (at & 31) & 1u;
+        const int entry = again && a.bias_offsets != nullptr ? sparse.bias[at] : 0;
+        const float bias = entry > 0 ? __ldg(a.bias_values + __ldg(a.bias_offsets + b) + entry - 1) : 0.f;
+#pragma unroll 4
+        for (int q = first + static_cast<int>(threadIdx.x) / wide; q < last; q += stride) {
+            const int side = q >= a.rows[0], r = q - (side ? a.rows[0] : 0);
+            const size_t line = (static_cast<size_t>(b) * a.rows[side] + r) * a.V;
+            const int s = static_cast<int>(reinterpret_cast<uintptr_t>(static_cast<const elem*>(a.in[side]) + line) % 16 / sizeof(elem));
+            if (static_cast<unsigned>(t + s - span * kIds) >= static_cast<unsigned>(kIds)) continue;      // (another block's, in this row)
+            elem* row = static_cast<elem*>(a.out[side]) + line;
+            int ctx = 0, d = 0;
+            if (again || allowed != nullptr) ctx = context_row(a, b, side, r);
+            if (again && a.penalties) d = drafted(a, b, ctx, t);
+            const bool may = allowed == nullptr || (__ldg(allowed + static_cast<size_t>(ctx) * a.W + (t >> 5)) >> (t & 31) & 1u);
+            // (as it was read: where the row is done in place the vectors left these as they were)
+            const float y = process_id(read_id<DT>(static_cast<const elem*>(a.in[side]) + line, t), count, d, bias, entry > 0, p);
+            write_id<DT>(row, t, may ? y : -INFINITY);
         }
     }
 }

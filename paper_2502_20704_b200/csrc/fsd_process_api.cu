@@ -65,20 +65,20 @@ CutShape cut_shape(const ProcArgs& a, bool raw) {
     return c;
 }
 
-// bf16: the shared memory of a block that does a row: the bins, and where there are sparse ids their bitmap and list, of 8192 of them if
-// two blocks an SM have room for it.  False where the vocabulary is too long for that.
+// bf16: the shared memory of a block that does a row: the bins, and where there are sparse ids their bitmap and list, of as many as two blocks
+// an SM have room for (16384 at most).  False where the vocabulary is too long for that.
 bool rows_shape(const ProcArgs& a, bool raw, RowsShape* shape, size_t* smem) {
     constexpr long long kTwo = 110 * 1024;                // what two blocks an SM may have each
     const bool sparse = !raw && a.penalties && (a.seen != nullptr || a.tokens != nullptr);
     shape->words = sparse ? (a.W + 3) / 4 * 4 : 0;
     shape->cap = 0;
-    const long long fixed = static_cast<long long>(kBins) * 4 + static_cast<long long>(shape->words) * 6;
+    const long long fixed = static_cast<long long>(kBins) * 4 + static_cast<long long>(shape->words) * 6;      // (a word and where its ids are in the list)
     if (sparse) {
-        const long long room = (fixed + 6 * 2048 <= kTwo ? kTwo : static_cast<long long>(kCutSmem)) - fixed;
-        if (room < 6 * 256) return false;
-        shape->cap = static_cast<int>(room / 6 < 8192 ? room / 6 / 8 * 8 : 8192);
+        const long long room = (fixed + 4 * 4096 <= kTwo ? kTwo : static_cast<long long>(kCutSmem)) - fixed;
+        if (room < 4 * 256) return false;
+        shape->cap = static_cast<int>(room / 4 < 16384 ? room / 16 * 4 : 16384);
     }
-    *smem = static_cast<size_t>(fixed) + static_cast<size_t>(shape->cap) * 6;
+    *smem = static_cast<size_t>(fixed) + static_cast<size_t>(shape->cap) * 4;
     return true;
 }
 
@@ -144,9 +144,10 @@ int launch(const ProcArgs& a, bool cut, cudaStream_t s) {
     if (cut && a.bias_offsets == nullptr && room) return launch_cut<DT>(a, false, s);
     // a row's vectors, wherever it starts, by blocks
     const long long spans = (a.V + 2 * (Logit<DT>::kPerVec - 1)) / Logit<DT>::kPerVec / kProcThreads + 1;
-    // as many rows a block as leave eight blocks an SM, so that the counts are read for many rows at once
+    // as many rows a block as leave eight blocks an SM, and four at least: what a block sets up is for all of them
     long long group = spans * a.B * all / (8 * kSMs);
-    group = group < 1 ? 1 : group > all ? all : group;
+    group = group < 4 ? 4 : group;
+    group = group > all ? all : group;
     const long long groups = (all + group - 1) / group;
     if (spans * groups * a.B > INT_MAX) return FSD_ERR_SHAPE;
     fsd_process_kernel<DT><<<static_cast<unsigned>(spans * groups * a.B), kProcThreads, 0, s>>>(a, static_cast<int>(spans), static_cast<int>(groups), static_cast<int>(group));

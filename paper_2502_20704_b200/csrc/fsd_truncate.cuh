@@ -275,6 +275,10 @@ struct CutResult {
     long long ties;
     uint32_t over;             // refining top-k: whether all that are equal to the k-th are kept
 };
+struct Run {
+    uint32_t n;
+    double w;
+};
 struct BinsShared {
     uint32_t mixed;            // whether the middle bin has more than zeros
     uint32_t under_lo, under_hi;       // keys of the lowest bin's values
@@ -284,7 +288,9 @@ struct BinsShared {
     uint32_t min_key;
     uint32_t settings[8];
     CutResult work;
-    int found[4];
+    int found[4], group[3];
+    Run before[3];
+    uint32_t place_n;
     double goal, above_goal;
 };
 __device__ __forceinline__ void clear_bins(uint32_t* hist, BinsShared& s) {
@@ -320,6 +326,16 @@ __device__ __noinline__ void count_value(uint32_t bits, uint32_t* hist, BinsShar
     }
     atomicAdd(&hist[bin], static_cast<uint32_t>(BY));
 }
+__device__ __forceinline__ uint32_t min_halves(uint32_t a, uint32_t b) {
+    uint32_t m;
+    asm("min.u16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
+    return m;
+}
+__device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) {
+    uint32_t m;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
+    return m;
+}
 // A vector of values into the bins.  bf16: two at a time, in halves of a word.
 template <int DT>
 __device__ __forceinline__ void count_vec(const uint4& v, uint32_t* hist, BinsShared* s) {
@@ -328,9 +344,9 @@ __device__ __forceinline__ void count_vec(const uint4& v, uint32_t* hist, BinsSh
         uint32_t bin[4], lowest = 0xffffffffu, highest = 0u;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const uint32_t m = __vminu2(__vmaxu2(w[k] & 0x7fff7fffu, kMagLo * 0x10001u), kMagHi * 0x10001u);
-            lowest = __vminu2(lowest, m);
-            highest = __vmaxu2(highest, m);
+            const uint32_t m = min_halves(max_halves(w[k] & 0x7fff7fffu, kMagLo * 0x10001u), kMagHi * 0x10001u);
+            lowest = min_halves(lowest, m);
+            highest = max_halves(highest, m);
             uint32_t sign;                                  // each half's sign in all of its bits
             asm("prmt.b32 %0, %1, 0, 0xbb99;" : "=r"(sign) : "r"(w[k]));
             bin[k] = (m - kMagLo * 0x10001u) ^ sign;
@@ -363,10 +379,6 @@ __device__ __forceinline__ void count_vec(const uint4& v, uint32_t* hist, BinsSh
 }
 
 // Exclusive sums over the threads of the block, in thread order.  All threads; ends with a barrier.
-struct Run {
-    uint32_t n;
-    double w;
-};
 __device__ __forceinline__ Run scan_threads(Run v, BinsShared& s, Run& all) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     Run t = v;
@@ -396,12 +408,48 @@ __device__ __forceinline__ Run scan_threads(Run v, BinsShared& s, Run& all) {
     return e;
 }
 
+// The bin in a thread's group of places at which a running sum gets to a goal, found by a warp, a place a lane.  `count`: the
+// sum is the number of tokens, else their weight.  Lanes without tokens are passed over; -1: it does not get there.
+struct PlaceFound {
+    int place;
+    uint32_t n;                // tokens in the bin
+    Run above;                 // what is above it
+    double w;                  // weight of each of its tokens
+};
+__device__ __forceinline__ PlaceFound find_place(const uint32_t* hist, int group, Run before, bool count, uint32_t n_goal, double w_goal) {
+    static_assert(kBinsEach <= 32, "a lane each");
+    const int lane = threadIdx.x & 31, place = group * kBinsEach + lane;
+    const bool is = lane < kBinsEach && place < kBins;
+    const uint32_t n = is ? hist[kBins - 1 - place] : 0u;
+    const double w = n != 0u ? __ldg(bin_weights + place) : 0.0;
+    Run run = {n, n * w};
+#pragma unroll
+    for (int d = 1; d < kBinsEach; d <<= 1) {
+        const uint32_t o = __shfl_up_sync(0xffffffffu, run.n, d);
+        const double p = __shfl_up_sync(0xffffffffu, run.w, d);
+        if (lane >= d) { run.n += o; run.w += p; }
+    }
+    const bool there = n != 0u && (count ? before.n + run.n >= n_goal : before.w + run.w >= w_goal);
+    const uint32_t ballot = __ballot_sync(0xffffffffu, there);
+    if (ballot == 0u) return {-1, 0u, before, 0.0};
+    const int at = __ffs(static_cast<int>(ballot)) - 1;
+    PlaceFound f;
+    f.place = group * kBinsEach + at;
+    f.n = __shfl_sync(0xffffffffu, n, at);
+    f.w = __shfl_sync(0xffffffffu, w, at);
+    f.above.n = before.n + __shfl_sync(0xffffffffu, run.n - n, at);
+    const double up_to = __shfl_sync(0xffffffffu, run.w, at > 0 ? at - 1 : 0);
+    f.above.w = at > 0 ? before.w + up_to : before.w;
+    return f;
+}
+
 // From the counts to the cut (bf16) or to the bins that hold the cuts (fp32).  `place` counts bins from the highest one down, a thread
 // has kBinsEach of them.  top: fp32, the largest key.  All of a block's threads; s.work has it behind the next barrier.
 template <int DT>
 __device__ __forceinline__ void solve_bins(const uint32_t* hist, BinsShared& s, const CutParams& c, int V, uint32_t top) {
-    const int tid = threadIdx.x, p0 = tid * kBinsEach;
+    const int tid = threadIdx.x, warp = tid >> 5, p0 = tid * kBinsEach;
     if (tid == 0) {
+        s.group[0] = s.group[1] = s.group[2] = kRowThreads;
         s.found[0] = -1;                                     // place of the k-th token
         s.found[1] = s.found[2] = kBins;                     // of the highest one, and of the border of top-p
         s.work = {kCutDone, 0u, V, 0u};
@@ -428,28 +476,31 @@ __device__ __forceinline__ void solve_bins(const uint32_t* hist, BinsShared& s, 
         if (tid == 0) s.work.kind = kCutNone;
         return;
     }
-    if (mine.n != 0u && (before.n == 0u || (cut_k && before.n < k && before.n + mine.n >= k))) {
-        Run run = before;
-#pragma unroll 1
-        for (int place = p0; place < p0 + kBinsEach && place < kBins; ++place) {
-            const int bin = kBins - 1 - place;
-            const uint32_t n = hist[bin];
-            if (n == 0u) continue;
-            const double w = bin_weights[place];
-            if (run.n == 0u) {
-                s.found[1] = place;
-                if (DT == FSD_BF16 && c.m && one_value(s, bin)) {
-                    const uint32_t key = bin_prefix<DT>(s, bin);
-                    s.min_key = min_p_key<DT>(c.min_p, key, value_of<DT>(key));
-                }
+    // the threads that have the highest bin, the k-th token and the border of top-p; a warp each looks for the bin
+    const auto has_goal = [&](double goal) { return mine.n != 0u && before.w < goal && !(before.w + mine.w < goal * (1.0 - 1e-9)); };   // (rounded in another order)
+    const auto tell = [&](int what) { s.group[what] = tid; s.before[what] = before; };
+    if (mine.n != 0u && before.n == 0u) tell(0);
+    if (cut_k && before.n < k && before.n + mine.n >= k) tell(1);
+    double goal = static_cast<double>(c.top_p) * all.w;
+    if (c.p && !cut_k && has_goal(goal)) atomicMin(&s.group[2], tid);
+    __syncthreads();
+    if (warp == 0) {
+        const PlaceFound f = find_place(hist, s.group[0], s.before[0], true, 1u, 0.0);
+        if (tid == 0) {
+            s.found[1] = f.place;
+            const int bin = kBins - 1 - f.place;
+            if (DT == FSD_BF16 && c.m && one_value(s, bin)) {
+                const uint32_t key = bin_prefix<DT>(s, bin);
+                s.min_key = min_p_key<DT>(c.min_p, key, value_of<DT>(key));
             }
-            if (cut_k && run.n < k && run.n + n >= k) {
-                s.found[0] = place;
-                s.work.ties = k - run.n;
-                s.goal = run.w + static_cast<double>(k - run.n) * w;
-            }
-            run.n += n;
-            run.w += n * w;
+        }
+    } else if (warp == 1 && cut_k) {
+        const PlaceFound f = find_place(hist, s.group[1], s.before[1], true, k, 0.0);
+        if ((tid & 31) == 0) {
+            s.found[0] = f.place;
+            s.work.ties = k - f.above.n;
+            s.goal = f.above.w + static_cast<double>(k - f.above.n) * f.w;
+            s.place_n = f.n;
         }
     }
     __syncthreads();
@@ -458,53 +509,62 @@ __device__ __forceinline__ void solve_bins(const uint32_t* hist, BinsShared& s, 
     const float most = DT == FSD_F32 ? value_of<FSD_F32>(top) : value_of<DT>(bin_prefix<DT>(s, top_bin));
     const bool off = hist[kBinOver] != 0u || !one_value(s, top_bin) || ((hist[kBinUnder] != 0u || top_bin == kBinUnder) && !(most >= -60.f)) ||
                      (cut_k && !one_value(s, k_bin));
-    const double goal = static_cast<double>(c.top_p) * (cut_k ? s.goal : all.w);
+    if (off) {
+        if (tid == 0) s.work.kind = kCutByBits;
+        return;
+    }
     int p_place = k_place;
-    if (c.p && !off) {                                       // the first place at which the tokens so far weigh the goal
-        if (mine.n != 0u && before.w < goal && !(before.w + mine.w < goal * (1.0 - 1e-9))) {       // (rounded in another order)
-            double run = before.w;
-#pragma unroll 1
-            for (int place = p0; place < p0 + kBinsEach && place < kBins; ++place) {
-                const uint32_t n = hist[kBins - 1 - place];
-                run += n * bin_weights[place];
-                if (n != 0u && run >= goal) { atomicMin(&s.found[2], place); break; }
+    uint32_t n_cut = cut_k ? s.place_n : 0u;                 // tokens in the bin of the cut
+    long long ties = s.work.ties;
+    if (c.p) {                                               // the first place at which the tokens so far weigh the goal
+        if (cut_k) {
+            goal = static_cast<double>(c.top_p) * s.goal;
+            if (has_goal(goal)) atomicMin(&s.group[2], tid);
+            __syncthreads();
+        }
+        const int first = s.group[2];
+        if (first < kRowThreads && tid / 32 == first / 32) { // (its own warp: s.before has one thread's)
+            const Run from = {__shfl_sync(0xffffffffu, before.n, first & 31), __shfl_sync(0xffffffffu, before.w, first & 31)};
+            PlaceFound f = find_place(hist, first, from, false, 0u, goal);
+            const double end = __shfl_sync(0xffffffffu, before.w + mine.w, first & 31);
+            if (f.place < 0 && first + 1 < kRowThreads)      // where two threads' sums meet: it starts the next group
+                f = find_place(hist, first + 1, {0u, end}, true, 1u, 0.0);
+            if ((tid & 31) == 0) {
+                if (f.place >= 0) s.found[2] = f.place;
+                s.before[2] = {f.n, f.above.w};
+                s.above_goal = f.w;
             }
         }
         __syncthreads();
         p_place = s.found[2];
-        if (p_place >= kBins) {                              // where two threads' sums meet: the first that starts at the goal
-            const int from = __reduce_min_sync(0xffffffffu, mine.n != 0u && before.w >= goal ? p0 : kBins);
-            __syncthreads();
-            if ((tid & 31) == 0 && from < kBins) atomicMin(&s.found[2], from);
-            __syncthreads();
-            p_place = s.found[2];
-            while (p_place < kBins && hist[kBins - 1 - p_place] == 0u) ++p_place;
-        }
-        if (cut_k && p_place > k_place) p_place = k_place;
         if (!(goal > 0.0)) p_place = s.found[1];
-        if (p_place >= kBins) p_place = kBins - 1;           // (not reached: the goal is below the whole)
+        if (cut_k && p_place > k_place) p_place = k_place;
+        const bool at_k = cut_k && p_place == k_place;
+        if (p_place == s.found[2]) {
+            n_cut = s.before[2].n;
+            const long long t = ties_below(s.before[2].w, s.above_goal, goal, V);
+            ties = at_k && ties < t ? ties : t;
+        } else if (!(goal > 0.0)) {
+            n_cut = hist[kBins - 1 - p_place];
+            ties = 1;
+        }
     }
     const int p_bin = kBins - 1 - p_place;
-    if (off || (c.p && !one_value(s, p_bin))) {
+    if (c.p && (p_bin < 0 || !one_value(s, p_bin))) {
+        __syncthreads();
         if (tid == 0) s.work.kind = kCutByBits;
         return;
     }
+    __syncthreads();                                         // (s.work.ties has been read)
+    if (tid != 0) return;
     if constexpr (DT == FSD_BF16) {
-        const bool has = (c.p || cut_k) && p_place / kBinsEach == tid;        // the thread that has the cut's bin
-        if (has) {
-            double above = before.w;
-#pragma unroll 1
-            for (int place = p0; place < p_place; ++place) above += hist[kBins - 1 - place] * bin_weights[place];
-            long long t = c.p ? ties_below(above, bin_weights[p_place], goal, V) : V;
-            if (cut_k && p_place == k_place && s.work.ties < t) t = s.work.ties;
-            s.work.ties = t >= hist[p_bin] ? V : t;                           // all of them
+        if (c.p || cut_k) {
+            s.work.ties = ties >= n_cut ? V : ties;          // all of them
             s.work.key = bin_prefix<DT>(s, p_bin);
         }
-        if (has || (!c.p && !cut_k && tid == 0)) {
-            if (s.min_key > s.work.key) { s.work.key = s.min_key; s.work.ties = V; }
-            if (s.work.key == 0u) s.work.kind = kCutNone;
-        }
-    } else if (tid == 0) {
+        if (s.min_key > s.work.key) { s.work.key = s.min_key; s.work.ties = V; }
+        if (s.work.key == 0u) s.work.kind = kCutNone;
+    } else {
         s.found[3] = p_bin;
         if (cut_k) {
             s.work.kind = kCutRefineK;

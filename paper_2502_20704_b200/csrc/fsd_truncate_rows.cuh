@@ -17,6 +17,8 @@ struct RowsShared {
     BinsShared cut;
     uint32_t equal[2][kRowWarps];
     int n_sparse;
+    uint32_t from;             // key of the smallest value read that comes to the cut
+    uint32_t some[8];          // the drafted ids' lowest 8 bits
 };
 
 __device__ __forceinline__ float value_at(const uint4& v, int e) {
@@ -32,15 +34,23 @@ __device__ __forceinline__ void put_at(uint4& v, int e, uint32_t half) {
     v.w = w == 3 ? __byte_perm(v.w, half, sel) : v.w;
 }
 
+// Whether any of a vector's values is at least `from`.
+__device__ __forceinline__ bool some_from(const uint4& v, const __nv_bfloat162& from) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t any = 0u;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) any |= __hge2_mask(*reinterpret_cast<const __nv_bfloat162*>(&w[k]), from);
+    return any != 0u;
+}
+
 __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const ProcArgs a, const RowsShape shape, bool raw) {
-    constexpr int DT = FSD_BF16, N = 8, kAtOnce = 4, kTile = kAtOnce * kRowThreads;
+    constexpr int DT = FSD_BF16, N = 8, kAtOnce = 2, kTile = kAtOnce * kRowThreads;
     extern __shared__ uint4 on_chip[];
     __shared__ RowsShared s;
     uint32_t* hist = reinterpret_cast<uint32_t*>(on_chip);
     uint32_t* bitmap = hist + kBins;                        // of the sparse ids
-    uint32_t* list = bitmap + shape.words;                  // them
-    uint16_t* becomes = reinterpret_cast<uint16_t*>(list + shape.cap);
-    uint16_t* ahead = becomes + shape.cap;                  // how many of them are in front of a word
+    uint32_t* list = bitmap + shape.words;                  // them, and then what becomes of them
+    uint16_t* ahead = reinterpret_cast<uint16_t*>(list + shape.cap);          // where in the list a word's are
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int all = a.rows[0] + a.rows[1], b = blockIdx.x / all, q = blockIdx.x % all;
     const int side = q >= a.rows[0], r = q - (side ? a.rows[0] : 0);
@@ -76,7 +86,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const Proc
     const uint32_t* seen = history ? a.seen + static_cast<size_t>(b) * a.W : nullptr;
     const uint32_t* allowed = !raw && a.allowed != nullptr ? a.allowed + (static_cast<size_t>(b) * (a.P + 1) + ctx) * a.W : nullptr;
     clear_bins(hist, s.cut);
-    if (tid < 8) s.cut.settings[tid] = setting;
+    if (tid < 8) { s.cut.settings[tid] = setting; s.some[tid] = 0u; }
     if (sparse) {
         for (int w = tid; w < a.W; w += kRowThreads) {
             uint32_t bits = history ? __ldg(seen + w) : 0u;
@@ -96,30 +106,33 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const Proc
     };
     // what becomes of a sparse id
     const auto value_of_id = [&](int t, float x, int count) {
-        return process_id(x, count, drafts > 0 ? drafted(a, b, ctx, t) : 0, 0.f, false, p);
+        const bool maybe = drafts > 0 && (s.some[t >> 5 & 7] >> (t & 31) & 1u);
+        return process_id(x, count, maybe ? drafted(a, b, ctx, t) : 0, 0.f, false, p);
     };
     bool listed = false;
     if (sparse) {
         if (drafts > 0) {
-            for (int j = ctx - 1 - tid; j >= 0 && a.parent == nullptr; j -= kRowThreads) {
+            const auto add = [&](int j) {
                 const int t = __ldg(a.tokens + static_cast<size_t>(b) * a.P + j);
-                if (t >= 0 && t < a.V && (allowed == nullptr || (__ldg(allowed + (t >> 5)) >> (t & 31) & 1u))) atomicOr(&bitmap[t >> 5], 1u << (t & 31));
+                if (t < 0 || t >= a.V || !(allowed == nullptr || (__ldg(allowed + (t >> 5)) >> (t & 31) & 1u))) return;
+                atomicOr(&bitmap[t >> 5], 1u << (t & 31));
+                atomicOr(&s.some[t >> 5 & 7], 1u << (t & 31));
+            };
+            if (a.parent == nullptr) {
+                for (int j = tid; j < ctx; j += kRowThreads) add(j);
+            } else if (tid == 0) {
+                for (int j = ctx - 1; j >= 0; j = node_before(a, b, j)) add(j);
             }
-            if (a.parent != nullptr && tid == 0)
-                for (int j = ctx - 1; j >= 0; j = node_before(a, b, j)) {
-                    const int t = __ldg(a.tokens + static_cast<size_t>(b) * a.P + j);
-                    if (t >= 0 && t < a.V && (allowed == nullptr || (__ldg(allowed + (t >> 5)) >> (t & 31) & 1u))) atomicOr(&bitmap[t >> 5], 1u << (t & 31));
-                }
             __syncthreads();
         }
-        const int each = (a.W + kRowThreads - 1) / kRowThreads, w0 = tid * each, w1 = w0 + each < a.W ? w0 + each : a.W;
+        // (a thread's words are kRowThreads apart: low ids are used far more often)
         Run mine = {0u, 0.0}, total;
-        for (int w = w0; w < w1; ++w) mine.n += __popc(bitmap[w]);
+        for (int w = tid; w < a.W; w += kRowThreads) mine.n += __popc(bitmap[w]);
         uint32_t n = scan_threads(mine, s.cut, total).n;
         listed = total.n <= static_cast<uint32_t>(shape.cap);                 // (else each vector works its own out)
         if (tid == 0) s.n_sparse = static_cast<int>(total.n);
         if (listed)
-            for (int w = w0; w < w1; ++w) {
+            for (int w = tid; w < a.W; w += kRowThreads) {
                 ahead[w] = static_cast<uint16_t>(n);
                 for (uint32_t todo = bitmap[w]; todo != 0u; todo &= todo - 1u) list[n++] = w * 32 + __ffs(static_cast<int>(todo)) - 1;
             }
@@ -134,7 +147,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const Proc
             todo &= todo - 1u;
             uint32_t half;
             if (listed) {
-                half = becomes[ahead[t >> 5] + __popc(bitmap[t >> 5] & ((1u << (t & 31)) - 1u))];
+                half = list[ahead[t >> 5] + __popc(bitmap[t >> 5] & ((1u << (t & 31)) - 1u))];
             } else {
                 const bool used = history && (__ldg(seen + (t >> 5)) >> (t & 31) & 1u);
                 half = pack_bf16(value_of_id(t, value_at(was, e), used ? __ldg(a.counts + static_cast<size_t>(b) * a.V + t) : -1), 0.f);
@@ -166,7 +179,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const Proc
                 const int count = used ? __ldg(a.counts + static_cast<size_t>(b) * a.V + t) : -1;
                 const float x = read_id<DT>(row, t);
                 const uint32_t was = pack_bf16(__fmul_rn(x, p.inv_temp), 0.f) & 0xffffu, now = pack_bf16(value_of_id(t, x, count), 0.f) & 0xffffu;
-                becomes[k] = static_cast<uint16_t>(now);
+                list[k] = now;
                 count_value<DT, 1>(now << 16, hist, &s.cut);
                 count_value<DT, -1>(was << 16, hist, &s.cut);
             }
@@ -179,10 +192,29 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const Proc
         for (int k = tid; k < n_sparse; k += kRowThreads) {
             const int t = list[k];
             const bool used = history && (__ldg(seen + (t >> 5)) >> (t & 31) & 1u);
-            becomes[k] = static_cast<uint16_t>(pack_bf16(value_of_id(t, read_id<DT>(in, t), used ? __ldg(a.counts + static_cast<size_t>(b) * a.V + t) : -1), 0.f));
+            list[k] = pack_bf16(value_of_id(t, read_id<DT>(in, t), used ? __ldg(a.counts + static_cast<size_t>(b) * a.V + t) : -1), 0.f);
         }
         __syncthreads();
     }
+
+    // Of processed values only those at or above the cut matter, and they rise with what was read: the smallest value that was read
+    // and comes to the cut says of most vectors that nothing in them is kept, without processing them.
+    if (res.kind == kCutDone && warp == 0) {
+        const float value = value_of<DT>(res.key);
+        const auto comes = [&](uint32_t key) { return __uint_as_float(pack_bf16(__fmul_rn(value_of<DT>(key), p.inv_temp), 0.f) << 16) >= value; };
+        uint32_t lo = key_of_value<DT>(-INFINITY), hi = key_of_value<DT>(INFINITY);        // hi does, lo does not
+        while (hi - lo > 1u) {
+            const uint32_t step = (hi - lo) / 33u + 1u, at = lo + step * (lane + 1u);
+            const uint32_t ballot = __ballot_sync(0xffffffffu, at >= hi || comes(at));
+            const uint32_t first = ballot != 0u ? __ffs(static_cast<int>(ballot)) - 1 : 32u;
+            const uint32_t old = lo;
+            if (first > 0u) lo = old + step * first;
+            if (old + step * (first + 1u) < hi) hi = old + step * (first + 1u);
+        }
+        if (lane == 0) s.from = hi;
+    }
+    __syncthreads();
+    const __nv_bfloat162 from = __bfloat162bfloat162(__float2bfloat16_rn(value_of<DT>(s.from)));
 
     // the row again, cut off
     const bool cut = res.kind == kCutDone;
@@ -196,8 +228,12 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const Proc
         for (int u = 0; u < kAtOnce; ++u) {
             const int i = vec_of(tile, u), t0 = i * N - lies;
             if (i >= n_vecs) break;
-            uint4 v = process(got[u], t0);
-            if (n_sparse > 0) v = patch(v, got[u], t0);
+            uint4 v = make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u);
+            const bool look = n_sparse > 0 && bits8(bitmap, t0, 4 * a.W) != 0u;
+            if (!cut || look || some_from(got[u], from)) {
+                v = process(got[u], t0);
+                if (look) v = patch(v, got[u], t0);
+            }
             got[u] = v;
             if (left > 0 && left != LLONG_MAX) equal += equal_in<DT>(v, value);
         }
