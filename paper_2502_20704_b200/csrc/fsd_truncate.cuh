@@ -249,7 +249,7 @@ constexpr int kRowWarps = kRowThreads / 32;
 constexpr uint32_t kMagLo = 0x337f, kMagHi = 0x4300;       // upper halves: just below 2^-24, and 2^7
 constexpr int kHalfBins = static_cast<int>(kMagHi - kMagLo) + 1;
 constexpr int kBins = 2 * kHalfBins;                       // negative magnitudes falling, then positive ones rising
-constexpr int kBinUnder = 0, kBinOver = kBins - 1, kBinMid = kHalfBins;
+constexpr int kBinUnder = 0, kBinOver = kBins - 1, kBinMid = kHalfBins, kBinNone = kHalfBins - 1;
 constexpr int kBinsEach = ((kBins + kRowThreads - 1) / kRowThreads + 3) / 4 * 4;
 static_assert(kBins % 4 == 0, "whole vectors of bins");
 
@@ -337,24 +337,31 @@ __device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) {
     return m;
 }
 // A vector of values into the bins.  bf16: two at a time, in halves of a word.
-template <int DT>
-__device__ __forceinline__ void count_vec(const uint4& v, uint32_t* hist, BinsShared* s) {
+// SKIP: but not those that `skip` has all bits set for; they go to a bin of no value, kBinNone, whose count means nothing.
+template <int DT, bool SKIP = false>
+__device__ __forceinline__ void count_vec(const uint4& v, uint32_t* hist, BinsShared* s, const uint4& skip = make_uint4(0u, 0u, 0u, 0u)) {
     if constexpr (DT == FSD_BF16) {
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w}, not_these[4] = {skip.x, skip.y, skip.z, skip.w};
         uint32_t bin[4], lowest = 0xffffffffu, highest = 0u;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const uint32_t m = min_halves(max_halves(w[k] & 0x7fff7fffu, kMagLo * 0x10001u), kMagHi * 0x10001u);
+            uint32_t m = min_halves(max_halves(w[k] & 0x7fff7fffu, kMagLo * 0x10001u), kMagHi * 0x10001u);
+            if (SKIP) m = (m & ~not_these[k]) | (((kMagLo + 1u) * 0x10001u) & not_these[k]);
             lowest = min_halves(lowest, m);
             highest = max_halves(highest, m);
             uint32_t sign;                                  // each half's sign in all of its bits
             asm("prmt.b32 %0, %1, 0, 0xbb99;" : "=r"(sign) : "r"(w[k]));
             bin[k] = (m - kMagLo * 0x10001u) ^ sign;
+            if (SKIP) bin[k] |= not_these[k];               // -1: kBinNone
         }
         if ((lowest & 0xffffu) == kMagLo || lowest >> 16 == kMagLo || (highest & 0xffffu) == kMagHi || highest >> 16 == kMagHi) {
 #pragma unroll 1
             for (int k = 0; k < 4; ++k) {
-                const uint32_t two = k < 2 ? (k < 1 ? v.x : v.y) : (k < 3 ? v.z : v.w);
+                uint32_t two = k < 2 ? (k < 1 ? v.x : v.y) : (k < 3 ? v.z : v.w);
+                if (SKIP) {
+                    const uint32_t no = k < 2 ? (k < 1 ? skip.x : skip.y) : (k < 3 ? skip.z : skip.w);
+                    two = (two & ~no) | (0xff80ff80u & no);
+                }
                 if (two == 0xff80ff80u) continue;
                 count_value<DT, 1>(two << 16, hist, s);
                 count_value<DT, 1>(two & 0xffff0000u, hist, s);
@@ -408,6 +415,15 @@ __device__ __forceinline__ Run scan_threads(Run v, BinsShared& s, Run& all) {
     return e;
 }
 
+// What takes the weight of a bin's edge next to zero to that of its middle, fp32's: e^(half its width), or one over that.
+template <int DT>
+__device__ __forceinline__ double to_middle(int bin) {
+    if constexpr (DT == FSD_BF16) return 1.0;
+    const int u = bin >= kHalfBins ? bin - kHalfBins : kHalfBins - 1 - bin;
+    const float half = __uint_as_float((kMagLo + static_cast<uint32_t>(u)) << 16 & 0x7f800000u) * (1.f / 256.f);
+    return bin == kBinMid ? 1.0 : static_cast<double>(ex2(bin >= kHalfBins ? half * kLog2e : -half * kLog2e));
+}
+
 // The bin in a thread's group of places at which a running sum gets to a goal, found by a warp, a place a lane.  `count`: the
 // sum is the number of tokens, else their weight.  Lanes without tokens are passed over; -1: it does not get there.
 struct PlaceFound {
@@ -416,12 +432,13 @@ struct PlaceFound {
     Run above;                 // what is above it
     double w;                  // weight of each of its tokens
 };
+template <int DT>
 __device__ __forceinline__ PlaceFound find_place(const uint32_t* hist, int group, Run before, bool count, uint32_t n_goal, double w_goal) {
     static_assert(kBinsEach <= 32, "a lane each");
     const int lane = threadIdx.x & 31, place = group * kBinsEach + lane;
     const bool is = lane < kBinsEach && place < kBins;
     const uint32_t n = is ? hist[kBins - 1 - place] : 0u;
-    const double w = n != 0u ? __ldg(bin_weights + place) : 0.0;
+    const double w = n != 0u ? __ldg(bin_weights + place) * to_middle<DT>(kBins - 1 - place) : 0.0;
     Run run = {n, n * w};
 #pragma unroll
     for (int d = 1; d < kBinsEach; d <<= 1) {
@@ -461,11 +478,11 @@ __device__ __forceinline__ void solve_bins(const uint32_t* hist, BinsShared& s, 
         const int bin = kBins - 4 - (p0 + j);
         if (bin < 0) break;
         const uint4 v = *reinterpret_cast<const uint4*>(hist + bin);
-        if ((v.x | v.y | v.z | v.w) != 0u) {                 // (fp32: as if all of a bin were at its edge next to zero)
+        if ((v.x | v.y | v.z | v.w) != 0u) {                 // (fp32: as if all of a bin were in its middle)
             const double2* w = reinterpret_cast<const double2*>(bin_weights + p0 + j);
             const double2 w0 = __ldg(w), w1 = __ldg(w + 1);
             mine.n += v.x + v.y + v.z + v.w;
-            mine.w += (v.w * w0.x + v.z * w0.y) + (v.y * w1.x + v.x * w1.y);
+            mine.w += ((v.w * w0.x + v.z * w0.y) + (v.y * w1.x + v.x * w1.y)) * to_middle<DT>(bin);
         }
     }
     Run all;
@@ -485,7 +502,7 @@ __device__ __forceinline__ void solve_bins(const uint32_t* hist, BinsShared& s, 
     if (c.p && !cut_k && has_goal(goal)) atomicMin(&s.group[2], tid);
     __syncthreads();
     if (warp == 0) {
-        const PlaceFound f = find_place(hist, s.group[0], s.before[0], true, 1u, 0.0);
+        const PlaceFound f = find_place<DT>(hist, s.group[0], s.before[0], true, 1u, 0.0);
         if (tid == 0) {
             s.found[1] = f.place;
             const int bin = kBins - 1 - f.place;
@@ -495,7 +512,7 @@ __device__ __forceinline__ void solve_bins(const uint32_t* hist, BinsShared& s, 
             }
         }
     } else if (warp == 1 && cut_k) {
-        const PlaceFound f = find_place(hist, s.group[1], s.before[1], true, k, 0.0);
+        const PlaceFound f = find_place<DT>(hist, s.group[1], s.before[1], true, k, 0.0);
         if ((tid & 31) == 0) {
             s.found[0] = f.place;
             s.work.ties = k - f.above.n;
@@ -525,10 +542,10 @@ __device__ __forceinline__ void solve_bins(const uint32_t* hist, BinsShared& s, 
         const int first = s.group[2];
         if (first < kRowThreads && tid / 32 == first / 32) { // (its own warp: s.before has one thread's)
             const Run from = {__shfl_sync(0xffffffffu, before.n, first & 31), __shfl_sync(0xffffffffu, before.w, first & 31)};
-            PlaceFound f = find_place(hist, first, from, false, 0u, goal);
+            PlaceFound f = find_place<DT>(hist, first, from, false, 0u, goal);
             const double end = __shfl_sync(0xffffffffu, before.w + mine.w, first & 31);
             if (f.place < 0 && first + 1 < kRowThreads)      // where two threads' sums meet: it starts the next group
-                f = find_place(hist, first + 1, {0u, end}, true, 1u, 0.0);
+                f = find_place<DT>(hist, first + 1, {0u, end}, true, 1u, 0.0);
             if ((tid & 31) == 0) {
                 if (f.place >= 0) s.found[2] = f.place;
                 s.before[2] = {f.n, f.above.w};

@@ -8,8 +8,8 @@ namespace fsd {
 // The block reads the row twice and keeps none of it: once to count its values, and again, from the L2 cache for the most part
 // (two blocks an SM have 90 MB of rows of 152064 on the way), to write it.  No block waits for another, which is what most of
 // a cluster's time went into: 64 x 17 x 152064 took 660 us that way.
-// Sparse ids, whose penalties the count leaves out at first, are listed in front: a bitmap of the row's, the sum of its bits up to each word, and for
-// each id what becomes of it, worked out once, one a thread, when what was counted for it is taken back.
+// Sparse ids, which the count of the others leaves out, are listed in front: a bitmap of the row's, the sum of its bits up to each word, and for
+// each id what becomes of it, worked out once, one a thread, and counted then.
 struct RowsShape {             // of the dynamic shared memory; the last two are in words and ids
     int words, cap;
 };
@@ -18,6 +18,7 @@ struct RowsShared {
     uint32_t equal[2][kRowWarps];
     int n_sparse;
     uint32_t from;             // key of the smallest value read that comes to the cut
+    int raised;                // whether a sparse id became more than it would be without
     uint32_t some[8];          // the drafted ids' lowest 8 bits
 };
 
@@ -70,6 +71,11 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const Proc
             if (i < n_vecs) got[u] = load_ids<DT>(in, t0, a.V, t0 >= 0 && t0 + N <= a.V);
         }
     };
+    uint4 now[kAtOnce];                                     // (while a tile is done the next one is on its way)
+    const auto take = [&]() {
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) now[u] = got[u];
+    };
     uint32_t setting = 0u;
     if (tid < 8) {                                          // the sequence's settings, all read at once
         const void* const at_b[8] = {a.top_k, a.top_p, a.min_p, raw ? nullptr : a.repetition, raw ? nullptr : a.frequency, raw ? nullptr : a.presence,
@@ -86,6 +92,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const Proc
     const uint32_t* seen = history ? a.seen + static_cast<size_t>(b) * a.W : nullptr;
     const uint32_t* allowed = !raw && a.allowed != nullptr ? a.allowed + (static_cast<size_t>(b) * (a.P + 1) + ctx) * a.W : nullptr;
     clear_bins(hist, s.cut);
+    if (tid == 0) s.raised = 0;
     if (tid < 8) { s.cut.settings[tid] = setting; s.some[tid] = 0u; }
     if (sparse) {
         for (int w = tid; w < a.W; w += kRowThreads) {
@@ -99,10 +106,10 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const Proc
     const CutParams c = cut_params(s.cut.settings, a.V);
     const SeqParams p = seq_params(s.cut.settings + 3);
     const bool cutting = c.k || c.p || c.m;
-    const auto process = [&](const uint4& v, int t0) {
+    const auto may_of = [&](int t0) {
         uint32_t may = allowed != nullptr ? bits8(allowed, t0, 4 * a.W) : 0xffu;
         if (t0 < 0 || t0 + N > a.V) may &= ids_of<N>(t0, a.V);                // (what is not in the row counts as masked)
-        return process_vec<DT>(v, may, p.inv_temp);
+        return may;
     };
     // what becomes of a sparse id
     const auto value_of_id = [&](int t, float x, int count) {
@@ -157,72 +164,109 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const Proc
         return v;
     };
 
-    CutResult res = {kCutNone, 0u, a.V, 0u};
-    if (cutting) {
-        for (int tile = 0; tile < n_vecs; tile += kTile) {
-            if (tile > 0) fetch(tile);
-#pragma unroll
-            for (int u = 0; u < kAtOnce; ++u) {
-                const int i = vec_of(tile, u), t0 = i * N - lies;
-                if (i >= n_vecs) break;
-                uint4 v = process(got[u], t0);
-                if (n_sparse > 0 && !listed) v = patch(v, got[u], t0);
-                count_vec<DT>(v, hist, &s.cut);
-            }
-        }
-        if (listed) {
-            const uint16_t* row = in;
-#pragma unroll 4
-            for (int k = tid; k < n_sparse; k += kRowThreads) {
-                const int t = list[k];
-                const bool used = history && (__ldg(seen + (t >> 5)) >> (t & 31) & 1u);
-                const int count = used ? __ldg(a.counts + static_cast<size_t>(b) * a.V + t) : -1;
-                const float x = read_id<DT>(row, t);
-                const uint32_t was = pack_bf16(__fmul_rn(x, p.inv_temp), 0.f) & 0xffffu, now = pack_bf16(value_of_id(t, x, count), 0.f) & 0xffffu;
-                list[k] = now;
-                count_value<DT, 1>(now << 16, hist, &s.cut);
-                count_value<DT, -1>(was << 16, hist, &s.cut);
-            }
-        }
-        __syncthreads();
-        solve_bins<DT>(hist, s.cut, c, a.V, 0u);
-        __syncthreads();
-        res = s.cut.work;
-    } else if (listed) {
+    if (listed) {
+#pragma unroll 2
         for (int k = tid; k < n_sparse; k += kRowThreads) {
             const int t = list[k];
             const bool used = history && (__ldg(seen + (t >> 5)) >> (t & 31) & 1u);
-            list[k] = pack_bf16(value_of_id(t, read_id<DT>(in, t), used ? __ldg(a.counts + static_cast<size_t>(b) * a.V + t) : -1), 0.f);
+            const float x = read_id<DT>(in, t);
+            const uint32_t is = pack_bf16(value_of_id(t, x, used ? __ldg(a.counts + static_cast<size_t>(b) * a.V + t) : -1), 0.f) & 0xffffu;
+            list[k] = is;
+            if (!(__uint_as_float(is << 16) <= __uint_as_float(pack_bf16(__fmul_rn(x, p.inv_temp), 0.f) << 16))) s.raised = 1;
+            if (cutting) count_value<DT, 1>(is << 16, hist, &s.cut);
         }
-        __syncthreads();
     }
-
-    // Of processed values only those at or above the cut matter, and they rise with what was read: the smallest value that was read
-    // and comes to the cut says of most vectors that nothing in them is kept, without processing them.
-    if (res.kind == kCutDone && warp == 0) {
-        const float value = value_of<DT>(res.key);
+    // The smallest value that was read and is processed to `value` or more: processed values rise with what was read.  A warp; into s.from.
+    const auto find_from = [&](float value) {
         const auto comes = [&](uint32_t key) { return __uint_as_float(pack_bf16(__fmul_rn(value_of<DT>(key), p.inv_temp), 0.f) << 16) >= value; };
         uint32_t lo = key_of_value<DT>(-INFINITY), hi = key_of_value<DT>(INFINITY);        // hi does, lo does not
         while (hi - lo > 1u) {
-            const uint32_t step = (hi - lo) / 33u + 1u, at = lo + step * (lane + 1u);
-            const uint32_t ballot = __ballot_sync(0xffffffffu, at >= hi || comes(at));
+            const uint32_t step = (hi - lo) / 33u + 1u, to = lo + step * (lane + 1u);
+            const uint32_t ballot = __ballot_sync(0xffffffffu, to >= hi || comes(to));
             const uint32_t first = ballot != 0u ? __ffs(static_cast<int>(ballot)) - 1 : 32u;
             const uint32_t old = lo;
             if (first > 0u) lo = old + step * first;
             if (old + step * (first + 1u) < hi) hi = old + step * (first + 1u);
         }
         if (lane == 0) s.from = hi;
+    };
+
+    CutResult res = {kCutNone, 0u, a.V, 0u};
+    if (cutting) {
+        // Of a row that keeps few tokens, two tiles say what is below the last of them: vectors of such values alone are passed over.
+        const bool few = c.k && c.top_k <= kTile && n_vecs >= 8 * kTile;
+        const bool leaving_out = listed || allowed != nullptr;
+        bool passing = false;
+        __nv_bfloat162 from = __bfloat162bfloat162(__float2bfloat16_rn(0.f));
+        for (int tile = 0; tile < n_vecs; tile += kTile) {
+            take();
+            if (tile + kTile < n_vecs) fetch(tile + kTile);
+            else fetch(0);                                  // (for the second time through)
+            if (few && tile == 2 * kTile) {
+                if (tid == 0) s.from = 0xffffffffu;
+                __syncthreads();
+                if (tid == 0) hist[kBinNone] = 0u;
+                __syncthreads();
+                Run mine = {0u, 0.0}, total;
+                for (int j = tid * kBinsEach; j < (tid + 1) * kBinsEach && j < kBins; ++j) mine.n += hist[kBins - 1 - j];
+                const uint32_t ahead_n = scan_threads(mine, s.cut, total).n, k = static_cast<uint32_t>(c.top_k);
+                if (tid == 0) s.cut.found[0] = -1;
+                __syncthreads();
+                if (total.n > k && ahead_n < k && ahead_n + mine.n >= k) {
+                    uint32_t run = ahead_n;
+                    int place = tid * kBinsEach;
+                    while ((run += hist[kBins - 1 - place]) < k) ++place;
+                    s.cut.found[0] = place;
+                }
+                __syncthreads();
+                const int bin = kBins - 1 - s.cut.found[0];
+                if (bin < kBins && bin != kBinOver && bin != kBinMid && bin != kBinUnder) {
+                    passing = true;
+                    if (warp == 0) find_from(value_of<DT>(bin_prefix<DT>(s.cut, bin)));
+                    __syncthreads();
+                    from = __bfloat162bfloat162(__float2bfloat16_rn(value_of<DT>(s.from)));
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                const int i = vec_of(tile, u), t0 = i * N - lies;
+                if (i >= n_vecs) break;
+                if (passing && !some_from(now[u], from)) continue;
+                uint32_t may = may_of(t0);
+                uint4 v = process_vec<DT>(now[u], may, p.inv_temp);
+                if (n_sparse > 0) {
+                    const uint32_t bits = bits8(bitmap, t0, 4 * a.W);
+                    if (listed) may &= ~bits;
+                    else if (bits != 0u) v = patch(v, now[u], t0);
+                }
+                // (not by vector: some of a warp's nearly always have a bit, and it would do both)
+                if (!leaving_out && may == 0xffu) count_vec<DT>(v, hist, &s.cut);
+                else if (may != 0u) count_vec<DT, true>(v, hist, &s.cut, spread_bits<DT>(~may));
+            }
+        }
+        __syncthreads();
+        if (tid == 0) hist[kBinNone] = 0u;
+        __syncthreads();
+        solve_bins<DT>(hist, s.cut, c, a.V, 0u);
+        __syncthreads();
+        res = s.cut.work;
     }
+    __syncthreads();
+
+    // Of processed values only those at or above the cut matter, and they rise with what was read: the smallest value that was read
+    // and comes to the cut says of most vectors that nothing in them is kept, without processing them.
+    if (res.kind == kCutDone && warp == 0) find_from(value_of<DT>(res.key));
     __syncthreads();
     const __nv_bfloat162 from = __bfloat162bfloat162(__float2bfloat16_rn(value_of<DT>(s.from)));
 
     // the row again, cut off
-    const bool cut = res.kind == kCutDone;
+    const bool cut = res.kind == kCutDone, look_at = !listed || s.raised != 0;
     const float value = value_of<DT>(res.key);
     long long left = cut && res.ties < a.V ? res.ties : LLONG_MAX;             // how many of the tokens equal to the cut are still kept
     int turn = 0;
     for (int tile = 0; tile < n_vecs; tile += kTile) {
-        if (tile > 0 || n_vecs > kTile || !cutting) fetch(tile);
+        take();
+        if (tile + kTile < n_vecs) fetch(tile + kTile);
         int equal = 0;
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
@@ -230,11 +274,11 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const Proc
             if (i >= n_vecs) break;
             uint4 v = make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u);
             const bool look = n_sparse > 0 && bits8(bitmap, t0, 4 * a.W) != 0u;
-            if (!cut || look || some_from(got[u], from)) {
-                v = process(got[u], t0);
-                if (look) v = patch(v, got[u], t0);
+            if (!cut || (look && look_at) || some_from(now[u], from)) {
+                v = process_vec<DT>(now[u], may_of(t0), p.inv_temp);
+                if (look) v = patch(v, now[u], t0);
             }
-            got[u] = v;
+            now[u] = v;
             if (left > 0 && left != LLONG_MAX) equal += equal_in<DT>(v, value);
         }
         int mine = INT_MAX;                                 // what of them is left for the warp's vectors
@@ -257,7 +301,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const Proc
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
             const int i = vec_of(tile, u), t0 = i * N - lies;
-            uint4 v = got[u];
+            uint4 v = now[u];
             if (cut) {
                 if (mine > 0 && mine != INT_MAX) {          // the one warp that the last of them is in
                     const int n = i < n_vecs ? equal_in<DT>(v, value) : 0;
