@@ -59,7 +59,7 @@ CutShape cut_shape(const ProcArgs& a, bool raw) {
     c.blocks = 1;
     while (c.blocks < kMaxCutCluster && (vecs > c.blocks * 4096ll || (rows * c.blocks < 2 * kSMs && vecs > c.blocks * 512ll))) c.blocks <<= 1;
     c.slice = (vecs + c.blocks - 1) / c.blocks;
-    const bool drafts = !raw && a.penalties && a.tokens != nullptr;
+    const bool drafts = !raw && a.penalties && a.tokens != nullptr && c.slice * N / 32 + 2 > kDraftedWords;
     c.smem = static_cast<size_t>(c.slice) * 16 + kBins * sizeof(uint32_t) + (drafts ? (static_cast<size_t>(c.slice) * N / 32 + 2) * sizeof(uint32_t) : 0);
     c.fits = c.smem <= kCutSmem;
     return c;

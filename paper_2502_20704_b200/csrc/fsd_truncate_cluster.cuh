@@ -9,6 +9,8 @@ namespace fsd {
 // counts (additions into its shared memory, whole numbers, so that their order does not matter), finds the bin of the cut and tells
 // the others; that bin is split twice more by 8 bits.
 constexpr int kMaxCutCluster = 8;
+constexpr int kListed = 96;
+constexpr int kDraftedWords = 768;     // of a slice's bitmap of drafted ids in the space that is there for other things later; longer ones have their own
 constexpr double kFixed = 4398046511104.0;                 // 2^42: weights of a bin's tokens as whole numbers
 
 struct CutShared : BinsShared {
@@ -16,10 +18,17 @@ struct CutShared : BinsShared {
     uint32_t top[kMaxCutCluster];
     int equal[kMaxCutCluster];
     CountAndWeight slots[2][kMaxCutCluster];
-    uint64_t sub_w[256];
-    uint32_t sub_n[256];
     CutResult told[2];         // what the first block told last, and the time before
-    uint16_t list[kRowWarps][256];
+    union {
+        struct {                                           // in front of everything else
+            uint16_t list[kRowWarps][kListed];             // sparse ids
+            uint32_t drafted[kDraftedWords];
+        };
+        struct {
+            uint32_t sub_n[256], part[3][256];             // of a bin's 256 parts: tokens, and their weights' digits
+            uint64_t sub_w[256];                           // the first block's: weights, of all blocks
+        };
+    };
 };
 
 struct RowSlice {
@@ -35,11 +44,13 @@ __device__ __forceinline__ void cluster_barrier() { cluster_arrive(); cluster_wa
 // Counts, by the 8 bits above `shift`, the tokens whose keys have the upper bits `prefix` and are above `over`; with weights also
 // what they weigh against the largest value of the bin's range (whole numbers of 1 / kFixed), and what all tokens above and below the
 // prefix weigh against `most`.  All into the first block's shared memory.
+// (Weights are added by their digits to the base 2^16: an addition of 64 bits in shared memory is a loop.  A slice has
+// fewer than 2^16 tokens, so that none of the three sums overflows.)
 template <bool WEIGHTS>
 __device__ void count_bits(const RowSlice& row, CutShared& s, CutShared& first, int rank, uint32_t prefix, int shift, uint32_t over, double most) {
     const int tid = threadIdx.x;
     if (rank != 0) {
-        for (int i = tid; i < 256; i += kRowThreads) { s.sub_n[i] = 0u; s.sub_w[i] = 0u; }
+        for (int i = tid; i < 256; i += kRowThreads) { s.sub_n[i] = 0u; s.part[0][i] = s.part[1][i] = s.part[2][i] = 0u; }
         __syncthreads();
     }
     const double edge = value_of<FSD_F32>(prefix << (shift + 8) | ((1u << (shift + 8)) - 1u));
@@ -50,18 +61,21 @@ __device__ void count_bits(const RowSlice& row, CutShared& s, CutShared& first, 
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const uint32_t k = key_of<FSD_F32>(bits[e]), high = k >> (shift + 8);
-            if (WEIGHTS && bits[e] != 0xff800000u && k > over) {
-                if (high != prefix) {
-                    const double w = exp_of(static_cast<double>(__uint_as_float(bits[e])) - most);
-                    if (high > prefix) above.w += w; else rest.w += w;
-                }
+            if (k <= over || bits[e] == 0xff800000u) continue;
+            if (!WEIGHTS) {
+                if (high == prefix) atomicAdd(&s.sub_n[k >> shift & 255u], 1u);
+                continue;
             }
-            if (high == prefix && k > over) {
+            const double w = exp_of(static_cast<double>(__uint_as_float(bits[e])) - (high == prefix ? edge : most));
+            if (high > prefix) above.w += w;
+            if (high < prefix) rest.w += w;
+            if (high == prefix) {
                 const uint32_t bin = k >> shift & 255u;
+                const unsigned long long fixed = __double2ull_rn(w * kFixed);
                 atomicAdd(&s.sub_n[bin], 1u);
-                if (WEIGHTS)
-                    atomicAdd(reinterpret_cast<unsigned long long*>(&s.sub_w[bin]),
-                              __double2ull_rn(exp_of(static_cast<double>(__uint_as_float(bits[e])) - edge) * kFixed));
+                atomicAdd(&s.part[0][bin], static_cast<uint32_t>(fixed) & 0xffffu);
+                atomicAdd(&s.part[1][bin], static_cast<uint32_t>(fixed >> 16) & 0xffffu);
+                atomicAdd(&s.part[2][bin], static_cast<uint32_t>(fixed >> 32));
             }
         }
     }
@@ -71,12 +85,13 @@ __device__ void count_bits(const RowSlice& row, CutShared& s, CutShared& first, 
         if (tid == 0) { first.above[rank] = above.w; first.rest[rank] = rest.w; }
     }
     __syncthreads();
-    if (rank != 0)
-        for (int i = tid; i < 256; i += kRowThreads)
-            if (s.sub_n[i] != 0u) {
-                atomicAdd(&first.sub_n[i], s.sub_n[i]);
-                if (WEIGHTS) atomicAdd(reinterpret_cast<unsigned long long*>(&first.sub_w[i]), static_cast<unsigned long long>(s.sub_w[i]));
-            }
+    for (int i = tid; i < 256; i += kRowThreads) {
+        if (WEIGHTS) {
+            const unsigned long long w = s.part[0][i] + (static_cast<unsigned long long>(s.part[1][i]) << 16) + (static_cast<unsigned long long>(s.part[2][i]) << 32);
+            if (w != 0ull) atomicAdd(reinterpret_cast<unsigned long long*>(&first.sub_w[i]), w);
+        }
+        if (rank != 0 && s.sub_n[i] != 0u) atomicAdd(&first.sub_n[i], s.sub_n[i]);
+    }
 }
 
 // The first block tells the others what it found, and clears the counts for the next time.  Two places in turn: a block may still
@@ -87,7 +102,7 @@ __device__ __forceinline__ CutResult tell_result(CutShared& s, cg::cluster_group
         const int tid = threadIdx.x;
         __syncthreads();
         if (tid < blocks) *cluster.map_shared_rank(&s.told[turn], tid) = s.work;
-        for (int i = tid; i < 256; i += kRowThreads) { s.sub_n[i] = 0u; s.sub_w[i] = 0u; }
+        for (int i = tid; i < 256; i += kRowThreads) { s.sub_n[i] = 0u; s.part[0][i] = s.part[1][i] = s.part[2][i] = 0u; s.sub_w[i] = 0u; }
     }
     cluster_barrier();
     return s.told[turn];
@@ -240,7 +255,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_cluster_kernel(const P
     extern __shared__ uint4 on_chip[];
     __shared__ CutShared s;
     uint32_t* hist = reinterpret_cast<uint32_t*>(on_chip + slice);
-    uint32_t* drafted_ids = hist + kBins;                   // a bit for each of the slice's ids, from a multiple of 32 on; where tokens are drafted
+    uint32_t* drafted_ids = slice * N / 32 + 2 <= kDraftedWords ? s.drafted : hist + kBins;      // a bit for each of the slice's ids, from a multiple of 32 on; where tokens are drafted
     cg::cluster_group cluster = cg::this_cluster();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int blocks = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
@@ -282,7 +297,6 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_cluster_kernel(const P
     clear_bins(hist, s);
     if (drafts > 0)
         for (int i = tid; i < n_words; i += kRowThreads) drafted_ids[i] = 0u;
-    for (int i = tid; i < 256; i += kRowThreads) { s.sub_n[i] = 0u; s.sub_w[i] = 0u; }
     if (tid < 8) s.settings[tid] = setting;
     __syncthreads();
     cluster_arrive();                                       // from here on others may add to the first block's counts
@@ -346,14 +360,14 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_cluster_kernel(const P
             }
             const int total = __shfl_sync(0xffffffffu, at, 31);
             at -= __popc(todo);
-            for (int base = 0; base < total; base += 256) {
-                while (todo != 0u && at < base + 256) {
+            for (int base = 0; base < total; base += kListed) {
+                while (todo != 0u && at < base + kListed) {
                     s.list[warp][at - base] = static_cast<uint16_t>(lane * 32 + __ffs(static_cast<int>(todo)) - 1);
                     todo &= todo - 1u;
                     ++at;
                 }
                 __syncwarp();
-                const int n = total - base < 256 ? total - base : 256;
+                const int n = total - base < kListed ? total - base : kListed;
 #pragma unroll 4
                 for (int k0 = 0; k0 < n; k0 += 32) {
                     const int k = k0 + lane, l = k < n ? s.list[warp][k] : 0;

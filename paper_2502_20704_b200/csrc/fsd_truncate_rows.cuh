@@ -141,7 +141,11 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const Proc
         if (listed)
             for (int w = tid; w < a.W; w += kRowThreads) {
                 ahead[w] = static_cast<uint16_t>(n);
-                for (uint32_t todo = bitmap[w]; todo != 0u; todo &= todo - 1u) list[n++] = w * 32 + __ffs(static_cast<int>(todo)) - 1;
+                const uint32_t used = history ? __ldg(seen + w) : 0u;
+                for (uint32_t todo = bitmap[w]; todo != 0u; todo &= todo - 1u) {
+                    const int e = __ffs(static_cast<int>(todo)) - 1;
+                    list[n++] = static_cast<uint32_t>(w * 32 + e) | (used >> e & 1u) << 31;
+                }
             }
     }
     __syncthreads();
@@ -165,12 +169,12 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const Proc
     };
 
     if (listed) {
-#pragma unroll 2
+#pragma unroll 4
         for (int k = tid; k < n_sparse; k += kRowThreads) {
-            const int t = list[k];
-            const bool used = history && (__ldg(seen + (t >> 5)) >> (t & 31) & 1u);
+            const uint32_t entry = list[k];                 // (its highest bit: the id is used)
+            const int t = static_cast<int>(entry & 0x7fffffffu), count = (entry >> 31) != 0u ? __ldg(a.counts + static_cast<size_t>(b) * a.V + t) : -1;
             const float x = read_id<DT>(in, t);
-            const uint32_t is = pack_bf16(value_of_id(t, x, used ? __ldg(a.counts + static_cast<size_t>(b) * a.V + t) : -1), 0.f) & 0xffffu;
+            const uint32_t is = pack_bf16(value_of_id(t, x, count), 0.f) & 0xffffu;
             list[k] = is;
             if (!(__uint_as_float(is << 16) <= __uint_as_float(pack_bf16(__fmul_rn(x, p.inv_temp), 0.f) << 16))) s.raised = 1;
             if (cutting) count_value<DT, 1>(is << 16, hist, &s.cut);
