@@ -5,8 +5,8 @@
 
 namespace fsd {
 
-constexpr int kHistThreads = 512;
-constexpr int kHistSpan = 8192;        // ids a block counts, in shared memory
+constexpr int kHistThreads = 1024;
+constexpr int kHistSpan = 11264;        // ids a block counts, in shared memory
 
 // A block per sequence and span of the vocabulary.  It looks through all of the sequence's tokens, which the L2 cache has after
 // the first block, so that nothing has to be cleared first and each count is written once.  Whole numbers: the order of
@@ -19,11 +19,13 @@ __global__ void __launch_bounds__(kHistThreads) fsd_history_build_kernel(const i
     for (int i = threadIdx.x; i < kHistSpan; i += kHistThreads) n[i] = 0;
     for (int i = threadIdx.x; i < kHistSpan / 32; i += kHistThreads) bits[i] = 0u;
     __syncthreads();
+#pragma unroll 8
     for (int i = __ldg(prompt_offsets + b) + static_cast<int>(threadIdx.x), end = __ldg(prompt_offsets + b + 1); i < end; i += kHistThreads) {
         const int t = __ldg(prompt_tokens + i), k = t - lo;
         if (t >= lo && t < V && k < kHistSpan) atomicOr(&bits[k >> 5], 1u << (k & 31));
     }
     if (output_offsets != nullptr)
+#pragma unroll 8
         for (int i = __ldg(output_offsets + b) + static_cast<int>(threadIdx.x), end = __ldg(output_offsets + b + 1); i < end; i += kHistThreads) {
             const int t = __ldg(output_tokens + i), k = t - lo;
             if (t >= lo && t < V && k < kHistSpan) {

@@ -35,13 +35,13 @@ __device__ __forceinline__ void put_at(uint4& v, int e, uint32_t half) {
     v.w = w == 3 ? __byte_perm(v.w, half, sel) : v.w;
 }
 
-// Whether any of a vector's values is at least `from`.
+// Whether any of a vector's values is at least `from`, or none (NaN: a row that holds one is to be found out).
 __device__ __forceinline__ bool some_from(const uint4& v, const __nv_bfloat162& from) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    uint32_t any = 0u;
+    uint32_t below = 0xffffffffu;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) any |= __hge2_mask(*reinterpret_cast<const __nv_bfloat162*>(&w[k]), from);
-    return any != 0u;
+    for (int k = 0; k < 4; ++k) below &= __hlt2_mask(*reinterpret_cast<const __nv_bfloat162*>(&w[k]), from);
+    return below != 0xffffffffu;
 }
 
 __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const ProcArgs a, const RowsShape shape, bool raw) {
@@ -198,7 +198,8 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const Proc
     CutResult res = {kCutNone, 0u, a.V, 0u};
     if (cutting) {
         // Of a row that keeps few tokens, two tiles say what is below the last of them: vectors of such values alone are passed over.
-        const bool few = c.k && c.top_k <= kTile && n_vecs >= 8 * kTile;
+        // (Not where sparse ids are not listed: they may become more than they were.)
+        const bool few = c.k && c.top_k <= kTile && n_vecs >= 8 * kTile && (n_sparse == 0 || listed);
         const bool leaving_out = listed || allowed != nullptr;
         bool passing = false;
         __nv_bfloat162 from = __bfloat162bfloat162(__float2bfloat16_rn(0.f));

@@ -175,6 +175,42 @@ def test_cut_rows_of_every_shape(shape, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V,share", [(100003, 0.02), (100003, 0.6), (60000, 1.0), (300001, 0.01)])
+def test_cut_long_rows_of_long_histories(V, share, dtype):
+    """Few and many used ids, drafted ones, penalties that lower and that raise."""
+    c = lg.Call(4, 2, V, dtype, ("pen", "temp", "k", "p", "m"), seed=29)
+    rng = np.random.default_rng(V)
+    used = rng.random((4, V)) < share
+    c.o["seen"], c.o["counts"] = lg.bits_of(used), (used * rng.integers(0, 4, (4, V))).astype(np.int32)
+    c.o["repetition"], c.o["frequency"] = np.array([1.2, 0.6, 1.1, 1.3], np.float32), np.array([0.2, -0.4, 0.1, 0.0], np.float32)
+    c.o["top_k"], c.o["top_p"] = np.array([50, 50, 0, 7], np.int32), np.array([0.9, 1.0, 0.8, 1.0], np.float32)
+    c.o["min_p"][:] = 0
+    _cut(c)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("odd", [float("nan"), float("inf")])
+def test_a_value_that_is_no_number_far_behind_in_a_row_of_which_few_are_kept(odd, dtype):
+    c = lg.Call(3, 0, 120000, dtype, ("k", "temp"), seed=32)
+    c.o["top_k"] = np.array([20, 20, 20], np.int32)
+    c.logits["target"][1, 0, 119000] = odd
+    got = _cut(c)["target"]
+    assert [(r > -float("inf")).sum().item() for r in got[[0, 2], 0]] == [20, 20] and (got[1, 0] > -float("inf")).sum().item() >= 119999
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_finite_values_of_masked_tokens(dtype):
+    """The type's lowest number, or a large negative one, in place of -inf: top_k then reaches into them."""
+    c = lg.Call(4, 0, 9001, dtype, ("k", "p"), seed=33)
+    x = c.logits["target"]
+    low = [torch.finfo(x.dtype).min, -1e9, -30000.0, -1e4]
+    for b in range(4):
+        x[b, 0, torch.arange(9001) % 300 != b] = low[b]
+    c.o["top_k"], c.o["top_p"] = np.array([50, 20, 9000, 31], np.int32), np.array([1.0, 0.9, 1.0, 0.999], np.float32)
+    _cut(c)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_equal_values_at_the_cut_are_kept_by_rising_id(dtype):
     V = 9000
     c = lg.Call(6, 0, V, dtype, ("k", "p"), seed=23)
