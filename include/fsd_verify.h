@@ -350,8 +350,11 @@ void fsd_default_process_opts(fsd_process_opts *opts);
  *   draft_in,  draft_out  [B, gamma,   V]  or both NULL
  *   draft_tokens [B, gamma] int32; NULL: drafted tokens do not count as used.  An id outside [0, V) counts for nothing.
  *   opts         host pointer; the struct is read during the call, the arrays it points to when the kernels run
- * The logits, masks and arrays as in the verify calls: row-major, contiguous, element-aligned; V at most 2^30.  The call needs no
- * workspace, waits for nothing on the device and can be captured in a CUDA graph after one ordinary call on that device.
+ * The logits, masks and arrays as in the verify calls: row-major, contiguous, element-aligned; V at most 2^30.  The call is one
+ * kernel, or two (biases together with top_k, top_p or min_p; rows that do not fit on chip).  It needs no workspace, and can be captured
+ * in a CUDA graph after one ordinary call on that device with the same logit type and with top_k, top_p or min_p set if the captured one has
+ * any: that one sets kernels' attributes and copies a table of 64 KB that they read to the device (and waits for that copy alone).
+ * Calls share nothing but that table, which stays as it is; outputs do not depend on the order in which a kernel's threads run.
  * Errors: FSD_ERR_NULL (a required pointer, or one of a group that goes together), FSD_ERR_SHAPE, FSD_ERR_ALIGN,
  * FSD_ERR_ENUM, FSD_ERR_UNSUPPORTED (an output overlaps an input that it is not the same as, or another output), FSD_ERR_CUDA. */
 int fsd_process_chain(const void *target_in, const void *draft_in, const int32_t *draft_tokens,

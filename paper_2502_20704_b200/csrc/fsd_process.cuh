@@ -240,14 +240,17 @@ __device__ __forceinline__ uint4 merge(const uint4& a, const uint4& b, const uin
     return make_uint4((a.x & ~of_b.x) | (b.x & of_b.x), (a.y & ~of_b.y) | (b.y & of_b.y), (a.z & ~of_b.z) | (b.z & of_b.z), (a.w & ~of_b.w) | (b.w & of_b.w));
 }
 
-// A block takes a span of the vocabulary, a vector a thread, for some rows of one sequence.  First the mask and the temperature,
-// a vector at a time, which leave the sparse ids as they were read; then these, one id a thread: few of a vector's ids are sparse, but
-// of a warp's 256 some always are, and a loop over a vector's own took 50 instructions a logit where this takes a few.  (Done in
-// a tile of four rows in shared memory instead, 64 x 17 x 152064 took 247 us and 16 x 11 x 32000 26 where this takes 236 and 21.)
-// Counts and biases are looked up once for all rows.
+// A block takes a span of the vocabulary, a vector a thread, for some rows of one sequence, so that counts and biases are looked up once
+// for all of them.  First the mask and the temperature, a vector at a time, which leave the sparse ids as they were read; then these, one
+// id a thread: few of a vector's ids are sparse, but of a warp's 256 some always are, and a loop over a vector's own took 50
+// instructions a logit.  Without sparse ids the kernel is bound by memory (64 x 17 x 152064 bf16: 115 us, 90% of the rate of a copy);
+// with them by their stores of two bytes each, which the L2 cache takes one by one (250 us with some 11000 used ids a sequence).
+// In a tile of four rows in shared memory instead these took 247 us, but 16 x 11 x 32000 26 where it is 19.
 // Vectors are aligned in memory and not in the vocabulary: where a row starts s ids behind a 16-byte boundary, vector v
 // covers ids N v - s and on, and a row whose output lies differently is stored an id at a time.
-template <int DT>
+// REGULAR: every row's input and output starts on such a boundary and is a whole number of vectors, so that none of this has to be looked
+// after (32 x 13 x 128256 with masks 79 -> 71 us).
+template <int DT, bool REGULAR>
 __global__ void __launch_bounds__(kProcThreads) fsd_process_kernel(const ProcArgs a, int spans, int groups, int group_rows) {
     constexpr int N = Logit<DT>::kPerVec, kIds = kProcThreads * N, kSpan = kIds + 32;
     using elem = typename Logit<DT>::elem;
@@ -273,19 +276,19 @@ __global__ void __launch_bounds__(kProcThreads) fsd_process_kernel(const ProcArg
         const size_t at = (static_cast<size_t>(b) * a.rows[side] + r0) * a.V;
         const elem* in = static_cast<const elem*>(a.in[side]) + at;
         elem* out = static_cast<elem*>(a.out[side]) + at;
-        const bool alike = (reinterpret_cast<uintptr_t>(in) ^ reinterpret_cast<uintptr_t>(out)) % 16 == 0;
+        const bool alike = REGULAR || (reinterpret_cast<uintptr_t>(in) ^ reinterpret_cast<uintptr_t>(out)) % 16 == 0;
         const int base = (span * kProcThreads + static_cast<int>(threadIdx.x)) * N;
         struct Row {                                        // a row's vector on the way
             uint4 v;
             uint32_t may;
         };
-        const auto first_id = [&](const elem* row) { return base - static_cast<int>(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(elem)); };
+        const auto first_id = [&](const elem* row) { return REGULAR ? base : base - static_cast<int>(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(elem)); };
         const auto fetch = [&](const elem* row, int r) {
             Row f = {make_uint4(0u, 0u, 0u, 0u), 0xffu};
             const int t0 = first_id(row);
             if (t0 < a.V) {
                 if (allowed != nullptr) f.may = bits8(allowed + static_cast<size_t>(context_row(a, b, side, r)) * a.W, t0, 4 * a.W);
-                f.v = load_ids<DT>(row, t0, a.V, t0 >= 0 && t0 + N <= a.V);
+                f.v = load_ids<DT>(row, t0, a.V, REGULAR || (t0 >= 0 && t0 + N <= a.V));
             }
             return f;
         };
@@ -302,7 +305,7 @@ __global__ void __launch_bounds__(kProcThreads) fsd_process_kernel(const ProcArg
                     if (t0 != keep_at) { keep = spread_bits<DT>(bits8(sparse.bits, t0 - lo, sizeof(sparse.bits))); keep_at = t0; }
                     y = merge(y, f.v, keep);
                 }
-                store_ids<DT>(out, t0, a.V, t0 >= 0 && t0 + N <= a.V && alike, y);
+                store_ids<DT>(out, t0, a.V, REGULAR || (t0 >= 0 && t0 + N <= a.V && alike), y);
             }
             out += a.V;
         }
@@ -322,7 +325,7 @@ __global__ void __launch_bounds__(kProcThreads) fsd_process_kernel(const ProcArg
         for (int q = first + static_cast<int>(threadIdx.x) / wide; q < last; q += stride) {
             const int side = q >= a.rows[0], r = q - (side ? a.rows[0] : 0);
             const size_t line = (static_cast<size_t>(b) * a.rows[side] + r) * a.V;
-            const int s = static_cast<int>(reinterpret_cast<uintptr_t>(static_cast<const elem*>(a.in[side]) + line) % 16 / sizeof(elem));
+            const int s = REGULAR ? 0 : static_cast<int>(reinterpret_cast<uintptr_t>(static_cast<const elem*>(a.in[side]) + line) % 16 / sizeof(elem));
             if (static_cast<unsigned>(t + s - span * kIds) >= static_cast<unsigned>(kIds)) continue;      // (another block's, in this row)
             elem* row = static_cast<elem*>(a.out[side]) + line;
             int ctx = 0, d = 0;

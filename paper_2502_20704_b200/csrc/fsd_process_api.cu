@@ -45,6 +45,13 @@ int check(const fsd_process_opts* o) {
     return FSD_OK;
 }
 
+// Whether every row starts on a 16-byte boundary and is a whole number of 16-byte vectors.
+bool regular(const ProcArgs& a, size_t es) {
+    bool is = a.V * es % 16 == 0;
+    for (int k = 0; k < 2; ++k) is = is && (a.rows[k] == 0 || (aligned(a.in[k], 16) && aligned(a.out[k], 16)));
+    return is;
+}
+
 // fp32: how a row lies in the shared memory of a cluster's blocks.
 struct CutShape {
     int blocks, slice;         // slice: vectors a block has
@@ -57,7 +64,7 @@ CutShape cut_shape(const ProcArgs& a, bool raw) {
     const long long rows = static_cast<long long>(a.B) * (a.rows[0] + a.rows[1]);
     const int vecs = (a.V + 2 * (N - 1)) / N;             // a row's, wherever it starts
     c.blocks = 1;
-    while (c.blocks < kMaxCutCluster && (vecs > c.blocks * 4096ll || (rows * c.blocks < 2 * kSMs && vecs > c.blocks * 512ll))) c.blocks <<= 1;
+    while (c.blocks < kMaxCutCluster && (vecs > c.blocks * 4096ll || (rows * c.blocks < 2 * kSMs && vecs > c.blocks * 2048ll))) c.blocks <<= 1;
     c.slice = (vecs + c.blocks - 1) / c.blocks;
     const bool drafts = !raw && a.penalties && a.tokens != nullptr && c.slice * N / 32 + 2 > kDraftedWords;
     c.smem = static_cast<size_t>(c.slice) * 16 + kBins * sizeof(uint32_t) + (drafts ? (static_cast<size_t>(c.slice) * N / 32 + 2) * sizeof(uint32_t) : 0);
@@ -93,7 +100,8 @@ int prepare_cut() {
     std::lock_guard<std::mutex> lock(mu);
     if (ready[dev]) return FSD_OK;
     if (cudaFuncSetAttribute(fsd_cut_cluster_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kCutSmem)) != cudaSuccess ||
-        cudaFuncSetAttribute(fsd_cut_rows_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kCutSmem)) != cudaSuccess)
+        cudaFuncSetAttribute(fsd_cut_rows_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kCutSmem)) != cudaSuccess ||
+        cudaFuncSetAttribute(fsd_cut_rows_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kCutSmem)) != cudaSuccess)
         return FSD_ERR_CUDA;
     fill_bin_weights(weights);
     if (cudaMemcpyToSymbol(bin_weights, weights, sizeof weights) != cudaSuccess) return FSD_ERR_CUDA;
@@ -111,7 +119,7 @@ int launch_cut(const ProcArgs& a, bool raw, cudaStream_t s) {
         RowsShape shape;
         size_t smem;
         if (!rows_shape(a, raw, &shape, &smem)) return FSD_ERR_SHAPE;
-        fsd_cut_rows_kernel<<<static_cast<unsigned>(rows), kRowThreads, smem, s>>>(a, shape, raw);
+        (regular(a, 2) ? fsd_cut_rows_kernel<true> : fsd_cut_rows_kernel<false>)<<<static_cast<unsigned>(rows), kRowThreads, smem, s>>>(a, shape, raw);
         return cudaGetLastError() == cudaSuccess ? FSD_OK : FSD_ERR_CUDA;
     } else {
         const CutShape c = cut_shape(a, raw);
@@ -150,7 +158,7 @@ int launch(const ProcArgs& a, bool cut, cudaStream_t s) {
     group = group > all ? all : group;
     const long long groups = (all + group - 1) / group;
     if (spans * groups * a.B > INT_MAX) return FSD_ERR_SHAPE;
-    fsd_process_kernel<DT><<<static_cast<unsigned>(spans * groups * a.B), kProcThreads, 0, s>>>(a, static_cast<int>(spans), static_cast<int>(groups), static_cast<int>(group));
+    (regular(a, sizeof(typename Logit<DT>::elem)) ? fsd_process_kernel<DT, true> : fsd_process_kernel<DT, false>)<<<static_cast<unsigned>(spans * groups * a.B), kProcThreads, 0, s>>>(a, static_cast<int>(spans), static_cast<int>(groups), static_cast<int>(group));
     if (cudaGetLastError() != cudaSuccess) return FSD_ERR_CUDA;
     return cut ? launch_cut<DT>(a, true, s) : FSD_OK;
 }

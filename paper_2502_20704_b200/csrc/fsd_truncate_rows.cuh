@@ -7,7 +7,9 @@ namespace fsd {
 
 // The block reads the row twice and keeps none of it: once to count its values, and again, from the L2 cache for the most part
 // (two blocks an SM have 90 MB of rows of 152064 on the way), to write it.  No block waits for another, which is what most of
-// a cluster's time went into: 64 x 17 x 152064 took 660 us that way.
+// a cluster's time went into: 64 x 17 x 152064 took 660 us that way and takes 273 (top_p; 352 with penalties and mixed settings).
+// What bounds it now is its instructions, some 300 for 8 logits: 8 additions to the bins and their addresses, the mask, the temperature
+// and the border once or twice.
 // Sparse ids, which the count of the others leaves out, are listed in front: a bitmap of the row's, the sum of its bits up to each word, and for
 // each id what becomes of it, worked out once, one a thread, and counted then.
 struct RowsShape {             // of the dynamic shared memory; the last two are in words and ids
@@ -44,6 +46,8 @@ __device__ __forceinline__ bool some_from(const uint4& v, const __nv_bfloat162& 
     return below != 0xffffffffu;
 }
 
+// REGULAR: rows start on 16-byte boundaries and are whole numbers of vectors.
+template <bool REGULAR>
 __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const ProcArgs a, const RowsShape shape, bool raw) {
     constexpr int DT = FSD_BF16, N = 8, kAtOnce = 2, kTile = kAtOnce * kRowThreads;
     extern __shared__ uint4 on_chip[];
@@ -58,8 +62,8 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const Proc
     const size_t at = (static_cast<size_t>(b) * a.rows[side] + r) * a.V;
     const uint16_t* in = static_cast<const uint16_t*>(raw ? a.out[side] : a.in[side]) + at;
     uint16_t* out = static_cast<uint16_t*>(a.out[side]) + at;
-    const int lies = static_cast<int>(reinterpret_cast<uintptr_t>(in) % 16 / 2);
-    const bool alike = (reinterpret_cast<uintptr_t>(in) ^ reinterpret_cast<uintptr_t>(out)) % 16 == 0;
+    const int lies = REGULAR ? 0 : static_cast<int>(reinterpret_cast<uintptr_t>(in) % 16 / 2);
+    const bool alike = REGULAR || (reinterpret_cast<uintptr_t>(in) ^ reinterpret_cast<uintptr_t>(out)) % 16 == 0;
     const int n_vecs = (a.V + lies + N - 1) / N;
     // a warp has kAtOnce runs of 32 vectors of a tile, one behind the other
     const auto vec_of = [&](int tile, int u) { return tile + (warp * kAtOnce + u) * 32 + lane; };
@@ -68,7 +72,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const Proc
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
             const int i = vec_of(tile, u), t0 = i * N - lies;
-            if (i < n_vecs) got[u] = load_ids<DT>(in, t0, a.V, t0 >= 0 && t0 + N <= a.V);
+            if (i < n_vecs) got[u] = load_ids<DT>(in, t0, a.V, REGULAR || (t0 >= 0 && t0 + N <= a.V));
         }
     };
     uint4 now[kAtOnce];                                     // (while a tile is done the next one is on its way)
@@ -108,7 +112,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const Proc
     const bool cutting = c.k || c.p || c.m;
     const auto may_of = [&](int t0) {
         uint32_t may = allowed != nullptr ? bits8(allowed, t0, 4 * a.W) : 0xffu;
-        if (t0 < 0 || t0 + N > a.V) may &= ids_of<N>(t0, a.V);                // (what is not in the row counts as masked)
+        if (!REGULAR && (t0 < 0 || t0 + N > a.V)) may &= ids_of<N>(t0, a.V);                // (what is not in the row counts as masked)
         return may;
     };
     // what becomes of a sparse id
@@ -323,7 +327,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const Proc
                     v = cut_vec<DT>(v, value, mine == 0);
                 }
             }
-            if (i < n_vecs) store_ids<DT>(out, t0, a.V, t0 >= 0 && t0 + N <= a.V && alike, v);
+            if (i < n_vecs) store_ids<DT>(out, t0, a.V, REGULAR || (t0 >= 0 && t0 + N <= a.V && alike), v);
         }
     }
     if (res.kind != kCutByBits) return;
