@@ -27,6 +27,21 @@ inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return na != 0 && nb != 0 && x < y + nb && y < x + na;
 }
+// The launch's own status: cudaGetLastError() may give what some earlier call of the process left there.
+template <typename... KArgs, typename... Args>
+int put(void (*kernel)(KArgs...), long long blocks, int threads, size_t smem, cudaStream_t s, int cluster, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(blocks), 1, 1);
+    cfg.blockDim = dim3(static_cast<unsigned>(threads), 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = static_cast<unsigned>(cluster); attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 0 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...) == cudaSuccess ? FSD_OK : FSD_ERR_CUDA;
+}
 inline int words(int V) { return (V + 31) / 32; }
 
 int check(const fsd_process_opts* o) {
@@ -119,26 +134,12 @@ int launch_cut(const ProcArgs& a, bool raw, cudaStream_t s) {
         RowsShape shape;
         size_t smem;
         if (!rows_shape(a, raw, &shape, &smem)) return FSD_ERR_SHAPE;
-        (regular(a, 2) ? fsd_cut_rows_kernel<true> : fsd_cut_rows_kernel<false>)<<<static_cast<unsigned>(rows), kRowThreads, smem, s>>>(a, shape, raw);
-        return cudaGetLastError() == cudaSuccess ? FSD_OK : FSD_ERR_CUDA;
+        return put(regular(a, 2) ? fsd_cut_rows_kernel<true> : fsd_cut_rows_kernel<false>, rows, kRowThreads, smem, s, 0, a, shape, raw);
     } else {
         const CutShape c = cut_shape(a, raw);
         if (rows * c.blocks > INT_MAX) return FSD_ERR_SHAPE;
-        if (!c.fits) {
-            fsd_cut_long_kernel<DT><<<static_cast<unsigned>(rows), kLongThreads, 0, s>>>(a);
-            return cudaGetLastError() == cudaSuccess ? FSD_OK : FSD_ERR_CUDA;
-        }
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(static_cast<unsigned>(rows * c.blocks), 1, 1);
-        cfg.blockDim = dim3(kRowThreads, 1, 1);
-        cfg.dynamicSmemBytes = c.smem;
-        cfg.stream = s;
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = static_cast<unsigned>(c.blocks); attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-        return cudaLaunchKernelEx(&cfg, fsd_cut_cluster_kernel, a, c.slice, raw) == cudaSuccess ? FSD_OK : FSD_ERR_CUDA;
+        if (!c.fits) return put(fsd_cut_long_kernel<DT>, rows, kLongThreads, 0, s, 0, a);
+        return put(fsd_cut_cluster_kernel, rows * c.blocks, kRowThreads, c.smem, s, c.blocks, a, c.slice, raw);
     }
 }
 
@@ -158,8 +159,9 @@ int launch(const ProcArgs& a, bool cut, cudaStream_t s) {
     group = group > all ? all : group;
     const long long groups = (all + group - 1) / group;
     if (spans * groups * a.B > INT_MAX) return FSD_ERR_SHAPE;
-    (regular(a, sizeof(typename Logit<DT>::elem)) ? fsd_process_kernel<DT, true> : fsd_process_kernel<DT, false>)<<<static_cast<unsigned>(spans * groups * a.B), kProcThreads, 0, s>>>(a, static_cast<int>(spans), static_cast<int>(groups), static_cast<int>(group));
-    if (cudaGetLastError() != cudaSuccess) return FSD_ERR_CUDA;
+    const int rc = put(regular(a, sizeof(typename Logit<DT>::elem)) ? fsd_process_kernel<DT, true> : fsd_process_kernel<DT, false>, spans * groups * a.B, kProcThreads, 0, s, 0,
+                       a, static_cast<int>(spans), static_cast<int>(groups), static_cast<int>(group));
+    if (rc != FSD_OK) return rc;
     return cut ? launch_cut<DT>(a, true, s) : FSD_OK;
 }
 
@@ -206,9 +208,7 @@ int append(const int32_t* tokens, const int32_t* path, const int32_t* accept_len
     for (const void* p : {static_cast<const void*>(tokens), static_cast<const void*>(path), static_cast<const void*>(accept_len),
                           static_cast<const void*>(next_token), static_cast<const void*>(counts), static_cast<const void*>(seen)})
         if (!aligned(p, 4)) return FSD_ERR_ALIGN;
-    fsd_history_append_kernel<<<static_cast<unsigned>((B + 3) / 4), 128, 0, static_cast<cudaStream_t>(stream)>>>(tokens, path, accept_len, next_token, B, P, width, V,
-                                                                                                             words(V), counts, seen);
-    return cudaGetLastError() == cudaSuccess ? FSD_OK : FSD_ERR_CUDA;
+    return put(fsd_history_append_kernel, (B + 3ll) / 4, 128, 0, static_cast<cudaStream_t>(stream), 0, tokens, path, accept_len, next_token, B, P, width, V, words(V), counts, seen);
 }
 
 }  // namespace
@@ -248,9 +248,8 @@ int fsd_history_build(const int32_t* prompt_offsets, const int32_t* prompt_token
     for (const void* p : {static_cast<const void*>(prompt_offsets), static_cast<const void*>(prompt_tokens), static_cast<const void*>(output_offsets),
                           static_cast<const void*>(output_tokens), static_cast<const void*>(counts), static_cast<const void*>(seen)})
         if (!aligned(p, 4)) return FSD_ERR_ALIGN;
-    fsd_history_build_kernel<<<static_cast<unsigned>(spans * B), kHistThreads, 0, static_cast<cudaStream_t>(stream)>>>(
-        prompt_offsets, prompt_tokens, output_offsets, output_tokens, V, words(V), static_cast<int>(spans), counts, seen);
-    return cudaGetLastError() == cudaSuccess ? FSD_OK : FSD_ERR_CUDA;
+    return put(fsd_history_build_kernel, spans * B, kHistThreads, 0, static_cast<cudaStream_t>(stream), 0, prompt_offsets, prompt_tokens, output_offsets, output_tokens, V,
+               words(V), static_cast<int>(spans), counts, seen);
 }
 
 int fsd_history_append_chain(const int32_t* draft_tokens, const int32_t* accept_len, const int32_t* next_token, int B, int gamma, int V,
