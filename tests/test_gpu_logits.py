@@ -392,3 +392,27 @@ def test_calls_in_a_graph_on_another_stream_and_two_at_once():
                 graphs[k].replay()
         torch.cuda.synchronize()
         assert all(torch.equal(x[s].cpu().view(torch.uint8), want[s].view(torch.uint8)) for x in outs for s in x)
+
+
+def test_an_error_that_an_earlier_call_left_behind_is_not_this_call_s():
+    """The runtime keeps a thread's last error until somebody asks for it.  Here a copy from memory that is registered in part
+    may leave one: the host-buffer call that wants the copy fails, the next call of another kind does not."""
+    c = lg.Call(2, 1, 500, "bf16", ("pen", "temp"), seed=34)
+    want = c.run()
+    pages = torch.zeros(4 * 4096, dtype=torch.uint8)
+    first = (pages.data_ptr() + 4095) // 4096 * 4096
+    rt = torch.cuda.cudart()
+    o = fsd.make_opts(dtype="bf16", T=0.1)
+    n = fsd.fsd_host_staging_bytes(1, 1, 64, o)
+    staging = torch.empty(n, dtype=torch.uint8, device="cuda")
+    host = torch.zeros(4096, dtype=torch.uint8).pin_memory()
+    at = [host.data_ptr() + 512 * k for k in range(8)]
+    assert int(rt.cudaHostRegister(first, 4096, 0)) == 0
+    try:
+        rc = fsd.fsd_verify_chain_host(first + 4096 - 40, at[1], at[2], at[3], at[4], 1, 1, 64, o, at[5], at[6], at[7], at[7] + 64, staging, n,
+                                       torch.cuda.current_stream().cuda_stream)
+        assert rc in (0, -7)
+        got = c.run()
+    finally:
+        assert int(rt.cudaHostUnregister(first)) == 0
+    assert all(torch.equal(got[s].view(torch.uint8), want[s].view(torch.uint8)) for s in got)
