@@ -269,6 +269,8 @@ def make_process_opts(dtype="bf16", **arrays) -> FsdProcessOpts:
         if name not in known:
             raise TypeError(f"make_process_opts() got an unexpected option {name!r}")
         if t is not None and not isinstance(t, int):
+            if not t.is_cuda:
+                raise ValueError(f"{name}: a tensor on the GPU is wanted, got one on {t.device}")
             kind = str(t.dtype).replace("torch.", "")
             if kind not in (("int32", "uint32") if name in whole else ("float32",)) or not t.is_contiguous():
                 raise ValueError(f"{name}: a contiguous {'int32' if name in whole else 'float32'} tensor is wanted, got {kind}"

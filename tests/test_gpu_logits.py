@@ -394,6 +394,14 @@ def test_calls_in_a_graph_on_another_stream_and_two_at_once():
         assert all(torch.equal(x[s].cpu().view(torch.uint8), want[s].view(torch.uint8)) for x in outs for s in x)
 
 
+def test_options_check_types_and_layouts_of_tensors():
+    on = dict(device="cuda")
+    for bad in (dict(top_k=torch.zeros(3, **on)), dict(top_p=torch.zeros(3, dtype=torch.float64, **on)), dict(counts=torch.zeros(4, 6, dtype=torch.int32, **on).t()),
+                dict(top_p=torch.zeros(3))):
+        with pytest.raises(ValueError):
+            fsd.make_process_opts(**bad)
+
+
 def test_an_error_that_an_earlier_call_left_behind_is_not_this_call_s():
     """The runtime keeps a thread's last error until somebody asks for it.  Here a copy from memory that is registered in part
     may leave one: the host-buffer call that wants the copy fails, the next call of another kind does not."""
