@@ -240,13 +240,13 @@ __global__ void __launch_bounds__(kLongThreads) fsd_cut_long_kernel(const ProcAr
 // ---- cuts by the counts of bins -----------------------------------------------------
 // Values are counted by the upper 16 bits of their single-precision form.  For bf16 a bin is one value, so that the counts alone say
 // where every cut is and what everything weighs, with one exponential for a bin, from a table, instead of one for a token; for
-// fp32 they say which bins to look into.  The bins are those of magnitudes from 2^-24 up to 2^7, one for what is smaller
-// (zeros; anything else there has the weight of 0 but for 6e-8 of it), one for what is below, as long as it is one value (a mask's
+// fp32 they say which bins to look into.  The bins are those of magnitudes from 2^-23 up to 2^8, one for what is smaller
+// (zeros; anything else there has the weight of 0 but for 1.2e-7 of it), one for what is below, as long as it is one value (a mask's
 // lowest number), and one for what is above.  Where a cut falls on a bin of several values, or something is above, the row is cut a
 // bit at a time.
 constexpr int kRowThreads = 512;
 constexpr int kRowWarps = kRowThreads / 32;
-constexpr uint32_t kMagLo = 0x337f, kMagHi = 0x4300;       // upper halves: just below 2^-24, and 2^7
+constexpr uint32_t kMagLo = 0x33ff, kMagHi = 0x4380;       // upper halves: just below 2^-23, and 2^8
 constexpr int kHalfBins = static_cast<int>(kMagHi - kMagLo) + 1;
 constexpr int kBins = 2 * kHalfBins;                       // negative magnitudes falling, then positive ones rising
 constexpr int kBinUnder = 0, kBinOver = kBins - 1, kBinMid = kHalfBins, kBinNone = kHalfBins - 1;
@@ -522,9 +522,9 @@ __device__ __forceinline__ void solve_bins(const uint32_t* hist, BinsShared& s, 
     }
     __syncthreads();
     const int k_place = s.found[0], k_bin = kBins - 1 - k_place, top_bin = kBins - 1 - s.found[1];
-    // What is below the bins is worth nothing beside a highest value of at least -60 (e^-68 of it each) and is nothing but a count.
+    // What is below the bins is worth nothing beside a highest value of at least -180 (e^-76 of it each) and is nothing but a count.
     const float most = DT == FSD_F32 ? value_of<FSD_F32>(top) : value_of<DT>(bin_prefix<DT>(s, top_bin));
-    const bool off = hist[kBinOver] != 0u || !one_value(s, top_bin) || ((hist[kBinUnder] != 0u || top_bin == kBinUnder) && !(most >= -60.f)) ||
+    const bool off = hist[kBinOver] != 0u || !one_value(s, top_bin) || ((hist[kBinUnder] != 0u || top_bin == kBinUnder) && !(most >= -180.f)) ||
                      (cut_k && !one_value(s, k_bin));
     if (off) {
         if (tid == 0) s.work.kind = kCutByBits;

@@ -211,6 +211,25 @@ def test_finite_values_of_masked_tokens(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("top", [100.0, 127.0, 128.0, 250.0, 256.0, 700.0, -130.0, -200.0, -260.0])
+def test_cut_rows_far_from_zero(top, dtype):
+    """As a low temperature makes them, on both sides of where the bins end."""
+    c = lg.Call(3, 0, 5003, dtype, ("k", "p", "m"), seed=35)
+    c.logits["target"].sub_(c.logits["target"].max(dim=-1, keepdim=True).values).mul_(4).add_(top)
+    c.o["top_k"], c.o["top_p"], c.o["min_p"] = np.array([0, 30, 0], np.int32), np.array([0.9, 0.8, 1.0], np.float32), np.array([0, 0, 0.01], np.float32)
+    _cut(c)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_cut_rows_of_log_probabilities_with_a_sure_token(dtype):
+    c = lg.Call(4, 0, 4001, dtype, ("k", "p"), seed=36)
+    x = c.logits["target"]
+    x.copy_(torch.log_softmax(x.double() + torch.where(torch.arange(4001) == 9, torch.tensor([8.0, 14.0, 22.0, 60.0]).view(4, 1, 1), 0.0), -1).to(x.dtype))
+    c.o["top_k"], c.o["top_p"] = np.array([0, 5, 0, 0], np.int32), np.array([0.999, 0.99, 0.9, 0.5], np.float32)
+    _cut(c)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_equal_values_at_the_cut_are_kept_by_rising_id(dtype):
     V = 9000
     c = lg.Call(6, 0, V, dtype, ("k", "p"), seed=23)
