@@ -425,7 +425,8 @@ __device__ __forceinline__ double to_middle(int bin) {
 }
 
 // The bin in a thread's group of places at which a running sum gets to a goal, found by a warp, a place a lane.  `count`: the
-// sum is the number of tokens, else their weight.  Lanes without tokens are passed over; -1: it does not get there.
+// sum is the number of tokens, else their weight.  Lanes without tokens are passed over; -1: it does not get there, and `above` is then what
+// it gets to.
 struct PlaceFound {
     int place;
     uint32_t n;                // tokens in the bin
@@ -448,7 +449,8 @@ __device__ __forceinline__ PlaceFound find_place(const uint32_t* hist, int group
     }
     const bool there = n != 0u && (count ? before.n + run.n >= n_goal : before.w + run.w >= w_goal);
     const uint32_t ballot = __ballot_sync(0xffffffffu, there);
-    if (ballot == 0u) return {-1, 0u, before, 0.0};
+    if (ballot == 0u)
+        return {-1, 0u, {before.n + __shfl_sync(0xffffffffu, run.n, kBinsEach - 1), before.w + __shfl_sync(0xffffffffu, run.w, kBinsEach - 1)}, 0.0};
     const int at = __ffs(static_cast<int>(ballot)) - 1;
     PlaceFound f;
     f.place = group * kBinsEach + at;
@@ -482,7 +484,8 @@ __device__ __forceinline__ void solve_bins(const uint32_t* hist, BinsShared& s, 
             const double2* w = reinterpret_cast<const double2*>(bin_weights + p0 + j);
             const double2 w0 = __ldg(w), w1 = __ldg(w + 1);
             mine.n += v.x + v.y + v.z + v.w;
-            mine.w += ((v.w * w0.x + v.z * w0.y) + (v.y * w1.x + v.x * w1.y)) * to_middle<DT>(bin);
+            mine.w += (v.w * w0.x * to_middle<DT>(bin + 3) + v.z * w0.y * to_middle<DT>(bin + 2)) +
+                      (v.y * w1.x * to_middle<DT>(bin + 1) + v.x * w1.y * to_middle<DT>(bin));
         }
     }
     Run all;
@@ -494,12 +497,15 @@ __device__ __forceinline__ void solve_bins(const uint32_t* hist, BinsShared& s, 
         return;
     }
     // the threads that have the highest bin, the k-th token and the border of top-p; a warp each looks for the bin
-    const auto has_goal = [&](double goal) { return mine.n != 0u && before.w < goal && !(before.w + mine.w < goal * (1.0 - 1e-9)); };   // (rounded in another order)
+    const auto tell_goal = [&](double goal) {                // the first whose tokens and those before weigh the goal
+        const uint32_t ballot = __ballot_sync(0xffffffffu, mine.n != 0u && before.w + mine.w >= goal);
+        if (ballot != 0u && (tid & 31) == 0) atomicMin(&s.group[2], tid + __ffs(static_cast<int>(ballot)) - 1);
+    };
     const auto tell = [&](int what) { s.group[what] = tid; s.before[what] = before; };
     if (mine.n != 0u && before.n == 0u) tell(0);
     if (cut_k && before.n < k && before.n + mine.n >= k) tell(1);
     double goal = static_cast<double>(c.top_p) * all.w;
-    if (c.p && !cut_k && has_goal(goal)) atomicMin(&s.group[2], tid);
+    if (c.p && !cut_k) tell_goal(goal);
     __syncthreads();
     if (warp == 0) {
         const PlaceFound f = find_place<DT>(hist, s.group[0], s.before[0], true, 1u, 0.0);
@@ -536,16 +542,15 @@ __device__ __forceinline__ void solve_bins(const uint32_t* hist, BinsShared& s, 
     if (c.p) {                                               // the first place at which the tokens so far weigh the goal
         if (cut_k) {
             goal = static_cast<double>(c.top_p) * s.goal;
-            if (has_goal(goal)) atomicMin(&s.group[2], tid);
+            tell_goal(goal);
             __syncthreads();
         }
         const int first = s.group[2];
         if (first < kRowThreads && tid / 32 == first / 32) { // (its own warp: s.before has one thread's)
             const Run from = {__shfl_sync(0xffffffffu, before.n, first & 31), __shfl_sync(0xffffffffu, before.w, first & 31)};
             PlaceFound f = find_place<DT>(hist, first, from, false, 0u, goal);
-            const double end = __shfl_sync(0xffffffffu, before.w + mine.w, first & 31);
-            if (f.place < 0 && first + 1 < kRowThreads)      // where two threads' sums meet: it starts the next group
-                f = find_place<DT>(hist, first + 1, {0u, end}, true, 1u, 0.0);
+            // (A bin's sum is rounded in another order here than the thread's, so that the goal may be in a later group.)
+            for (int g = first + 1; f.place < 0 && g < kRowThreads; ++g) f = find_place<DT>(hist, g, f.above, false, 0u, goal);
             if ((tid & 31) == 0) {
                 if (f.place >= 0) s.found[2] = f.place;
                 s.before[2] = {f.n, f.above.w};

@@ -1,0 +1,40 @@
+"""Borders of top-p that are decided by little: rows in which one weight or its rounding says where the cut is."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import fsd_logits_oracle as lo
+from tests import logits as lg
+
+pytestmark = pytest.mark.gpu
+
+
+def _kept(rows, dtype, top_p, top_k=None):
+    """rows: a list a sequence of (value, how many).  How many tokens of each sequence are kept, next to what the oracle keeps."""
+    V = max(sum(n for _, n in r) for r in rows)
+    c = lg.Call(len(rows), 0, V, dtype, (), seed=40)
+    for b, r in enumerate(rows):
+        x = torch.cat([torch.full((n,), v, dtype=torch.float64) for v, n in r])
+        x = torch.nn.functional.pad(x, (0, V - x.numel()), value=-float("inf"))
+        c.logits["target"][b, 0] = x[torch.randperm(V, generator=torch.Generator().manual_seed(b))].to(lg.TORCH[dtype])
+    c.o["top_p"] = np.array(top_p, np.float32)
+    c.o["top_k"] = None if top_k is None else np.array(top_k, np.int32)
+    got = c.run()["target"]
+    for b in range(len(rows)):
+        y = c.logits["target"][b, 0]
+        keep = lo.kept(y.double().numpy(), None if top_k is None else top_k[b], c.o["top_p"][b].item())
+        want = torch.where(torch.from_numpy(keep), y, torch.tensor(-float("inf"), dtype=y.dtype))
+        assert torch.equal(got[b, 0], want), (b, int((got[b, 0] > -float("inf")).sum()), int(keep.sum()))
+    return [int((r > -float("inf")).sum()) for r in got[:, 0]]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_share_that_ends_just_behind_many_light_tokens(dtype):
+    """The tokens behind a sure one weigh 3e-10 of it each, so that what is missing at the end of some run of values is less than
+    1e-9 of the share and is still several tokens."""
+    light = [(-13.75, 10), (-13.8125, 1), (-13.875, 316453)]
+    assert _kept([[(8.0, 1)] + light], dtype, [0.9999]) == [14]
+    rows = [[(8.0, 1), (-13.75, 10), (-13.8125, k), (-13.875, 316453)] for k in range(1, 9)]
+    _kept(rows, dtype, [0.9999] * 8)
+    _kept(rows, dtype, [0.9999] * 8, [316000] * 8)
