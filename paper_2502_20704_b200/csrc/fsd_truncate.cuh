@@ -241,9 +241,9 @@ __global__ void __launch_bounds__(kLongThreads) fsd_cut_long_kernel(const ProcAr
 // Values are counted by the upper 16 bits of their single-precision form.  For bf16 a bin is one value, so that the counts alone say
 // where every cut is and what everything weighs, with one exponential for a bin, from a table, instead of one for a token; for
 // fp32 they say which bins to look into.  The bins are those of magnitudes from 2^-23 up to 2^8, one for what is smaller
-// (zeros; anything else there has the weight of 0 but for 1.2e-7 of it), one for what is below, as long as it is one value (a mask's
-// lowest number), and one for what is above.  Where a cut falls on a bin of several values, or something is above, the row is cut a
-// bit at a time.
+// (zeros; anything else there has the weight of 0 but for 2^-23), one for what is below, as long as it is one value (a mask's
+// lowest number), and one for what is above.  Where a cut falls on a bin of several values, where it would be another one with the smaller
+// values' weights each off by 2^-23, or where something is above, the row is cut a bit at a time.
 constexpr int kRowThreads = 512;
 constexpr int kRowWarps = kRowThreads / 32;
 constexpr uint32_t kMagLo = 0x33ff, kMagHi = 0x4380;       // upper halves: just below 2^-23, and 2^8
@@ -280,7 +280,7 @@ struct Run {
     double w;
 };
 struct BinsShared {
-    uint32_t mixed;            // whether the middle bin has more than zeros
+    uint32_t mixed;            // how many of the middle bin's are no zeros
     uint32_t under_lo, under_hi;       // keys of the lowest bin's values
     CountAndWeight scratch[32];
     uint32_t warp_n[kRowWarps];
@@ -316,7 +316,7 @@ __device__ __noinline__ void count_value(uint32_t bits, uint32_t* hist, BinsShar
     int bin = static_cast<int>(u ^ static_cast<uint32_t>(static_cast<int>(bits) >> 31)) + kHalfBins;
     if (u == 0u) {
         bin = kBinMid;
-        if (BY > 0 && (bits & 0x7fffffffu) != 0u) s->mixed = 1u;
+        if (BY > 0 && (bits & 0x7fffffffu) != 0u) atomicAdd(&s->mixed, 1u);
     }
     if ((bits & 0x7fffffffu) > 0x7f800000u) bin = kBinOver;
     if (BY > 0 && bin == kBinUnder) {
@@ -539,6 +539,7 @@ __device__ __forceinline__ void solve_bins(const uint32_t* hist, BinsShared& s, 
     int p_place = k_place;
     uint32_t n_cut = cut_k ? s.place_n : 0u;                 // tokens in the bin of the cut
     long long ties = s.work.ties;
+    bool sure = true;                                        // whether the border is there whatever the values next to zero weigh
     if (c.p) {                                               // the first place at which the tokens so far weigh the goal
         if (cut_k) {
             goal = static_cast<double>(c.top_p) * s.goal;
@@ -565,14 +566,20 @@ __device__ __forceinline__ void solve_bins(const uint32_t* hist, BinsShared& s, 
         if (p_place == s.found[2]) {
             n_cut = s.before[2].n;
             const long long t = ties_below(s.before[2].w, s.above_goal, goal, V);
-            ties = at_k && ties < t ? ties : t;
+            const bool all_of_k = at_k && ties <= t;
+            ties = all_of_k ? ties : t;
+            if (DT == FSD_BF16 && s.mixed != 0u && goal > 0.0) {              // (fp32's sums are of what each token weighs)
+                const double off = static_cast<double>(s.mixed) * 0x1p-23;
+                sure = (s.before[2].w == 0.0 && ties == 1) || s.before[2].w + static_cast<double>(ties - 1) * s.above_goal < goal - off;
+                sure = sure && (all_of_k || s.before[2].w + static_cast<double>(ties) * s.above_goal >= goal + off);
+            }
         } else if (!(goal > 0.0)) {
             n_cut = hist[kBins - 1 - p_place];
             ties = 1;
         }
     }
     const int p_bin = kBins - 1 - p_place;
-    if (c.p && (p_bin < 0 || !one_value(s, p_bin))) {
+    if (c.p && (p_bin < 0 || !one_value(s, p_bin) || !sure)) {
         __syncthreads();
         if (tid == 0) s.work.kind = kCutByBits;
         return;

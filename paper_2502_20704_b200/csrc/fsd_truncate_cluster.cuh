@@ -412,7 +412,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_cluster_kernel(const P
         for (int w = 0; w < kRowWarps; ++w) top = top > s.warp_n[w] ? top : s.warp_n[w];
         first.top[rank] = top;
         if (rank != 0) {
-            if (s.mixed != 0u) atomicOr(&first.mixed, 1u);
+            if (s.mixed != 0u) atomicAdd(&first.mixed, s.mixed);
             if (s.under_lo <= s.under_hi) { atomicMin(&first.under_lo, s.under_lo); atomicMax(&first.under_hi, s.under_hi); }
         }
     }

@@ -38,3 +38,22 @@ def test_a_share_that_ends_just_behind_many_light_tokens(dtype):
     rows = [[(8.0, 1), (-13.75, 10), (-13.8125, k), (-13.875, 316453)] for k in range(1, 9)]
     _kept(rows, dtype, [0.9999] * 8)
     _kept(rows, dtype, [0.9999] * 8, [316000] * 8)
+
+
+TINY = float(torch.tensor([0x33FE], dtype=torch.int16).view(torch.bfloat16).float())       # 1.18e-7
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("top_k", [None, 152065])
+def test_values_next_to_zero_weigh_what_they_weigh(top_k, dtype):
+    """A hundred thousand of 1.18e-7 weigh 0.01 tokens more than as many zeros."""
+    rows, share, k = [], [], None
+    rows.append([(1.0, 1), (TINY, 100000), (-1.0, 52064)]); share.append(0.8541399836540222)
+    rows.append([(1.0, 60000), (-TINY, 92064)]); share.append(0.3000155985355377)
+    for p in np.linspace(0.85, 0.97, 14):
+        rows.append([(1.0, 1), (TINY, 100000), (-1.0, 52064)]); share.append(p)
+    if top_k is not None:
+        k = [top_k - 1 - 64 * i for i in range(len(rows))]
+    got = _kept(rows, dtype, share, k)
+    if top_k is None:
+        assert got[:2] == [104821, 28162]
