@@ -565,7 +565,11 @@ __device__ __forceinline__ void solve_bins(const uint32_t* hist, BinsShared& s, 
         const bool at_k = cut_k && p_place == k_place;
         if (p_place == s.found[2]) {
             n_cut = s.before[2].n;
-            const long long t = ties_below(s.before[2].w, s.above_goal, goal, V);
+            // Where one value has all of the weight its tokens are counted, for a share may end on one of them exactly (of a thousand
+            // equal ones three quarters are 750), which 750 times a rounded weight does not.
+            const double equal = cut_k && at_k ? static_cast<double>(k) : static_cast<double>(n_cut);
+            const bool alone = DT == FSD_BF16 && goal > 0.0 && s.before[2].w == 0.0 && (cut_k ? s.goal : all.w) == equal * s.above_goal;
+            const long long t = alone ? ties_below(0.0, 1.0, static_cast<double>(c.top_p) * equal, V) : ties_below(s.before[2].w, s.above_goal, goal, V);
             const bool all_of_k = at_k && ties <= t;
             ties = all_of_k ? ties : t;
             if (DT == FSD_BF16 && s.mixed != 0u && goal > 0.0) {              // (fp32's sums are of what each token weighs)

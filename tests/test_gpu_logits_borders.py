@@ -57,3 +57,22 @@ def test_values_next_to_zero_weigh_what_they_weigh(top_k, dtype):
     got = _kept(rows, dtype, share, k)
     if top_k is None:
         assert got[:2] == [104821, 28162]
+
+
+@pytest.mark.parametrize("dtype", ["bf16"])
+@pytest.mark.parametrize("n", [100, 1000, 8192, 40000])
+def test_shares_of_equal_tokens_that_end_on_a_token(n, dtype):
+    """Of n equal tokens a share of k / n in 32 bits' fractions keeps k: the predecessors of the next one have the share, not less."""
+    values = [0.0625, 0.125, 0.25, -7.8125, -5.875, -3.125, 1.25, 7.5, 12.0, -20.0]
+    for p in (0.25, 0.5, 0.75):
+        assert _kept([[(v, n)] for v in values], dtype, [p] * len(values)) == [int(p * n)] * len(values)
+
+
+@pytest.mark.parametrize("dtype", ["bf16"])
+def test_shares_of_equal_tokens_in_front_of_others(dtype):
+    values = [0.0625, 0.125, -7.8125, -5.875, -3.125, 1.25, 7.5, 12.0]
+    # some that top_k leaves out, some below all bins, some that weigh e^-40 of the others
+    assert _kept([[(v, 1000), (v - 1.0, 5000)] for v in values], dtype, [0.75] * 8, [1000] * 8) == [750] * 8
+    assert _kept([[(v, 1000), (v - 1.0, 5000)] for v in values], dtype, [0.75] * 8, [100] * 8) == [75] * 8
+    assert _kept([[(v, 1000), (-30000.0, 5000)] for v in values], dtype, [0.75] * 8) == [750] * 8
+    assert _kept([[(v, 1000), (v - 40.0, 50)] for v in values], dtype, [0.75] * 8) == [750] * 8
