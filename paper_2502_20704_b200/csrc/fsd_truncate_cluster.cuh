@@ -7,12 +7,12 @@ namespace fsd {
 
 // A block reads its slice of the row once, processes it, keeps it in shared memory and counts it.  The first block of the cluster gets all
 // counts (additions into its shared memory, whole numbers, so that their order does not matter), finds the bin of the cut and tells
-// the others; that bin is split twice more by 8 bits.
+// the others; that bin is split twice more, by 8 bits and 8 for top-k, by 7 and 9 for top-p.
 // 64 x 17 x 152064 takes 1.9 ms, 1 x 32000 17 us: a dozen steps a row that each wait for the slowest block, with two blocks an SM.
 constexpr int kMaxCutCluster = 8;
 constexpr int kListed = 96;
 constexpr int kDraftedWords = 768;     // of a slice's bitmap of drafted ids in the space that is there for other things later; longer ones have their own
-constexpr double kFixed = 4398046511104.0;                 // 2^42: weights of a bin's tokens as whole numbers
+constexpr double kFixed = 18014398509481984.0;             // 2^54: weights of a bin's tokens as whole numbers
 
 struct CutShared : BinsShared {
     double above[kMaxCutCluster], rest[kMaxCutCluster];
@@ -26,8 +26,9 @@ struct CutShared : BinsShared {
             uint32_t drafted[kDraftedWords];
         };
         struct {
-            uint32_t sub_n[256], part[3][256];             // of a bin's 256 parts: tokens, and their weights' digits
-            uint64_t sub_w[256];                           // the first block's: weights, of all blocks
+            uint32_t sub_n[512];                           // of a bin's parts: tokens
+            uint32_t digits[4 * 128];                      // and, of 128 parts, their weights' digits
+            uint64_t sub_w[2 * 128];                       // the first block's: weights, of all blocks, their lower 32 bits and the rest
         };
     };
 };
@@ -42,56 +43,78 @@ __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 __device__ __forceinline__ void cluster_barrier() { cluster_arrive(); cluster_wait(); }
 
-// Counts, by the 8 bits above `shift`, the tokens whose keys have the upper bits `prefix` and are above `over`; with weights also
-// what they weigh against the largest value of the bin's range (whole numbers of 1 / kFixed), and what all tokens above and below the
-// prefix weigh against `most`.  All into the first block's shared memory.
-// (Weights are added by their digits to the base 2^16: an addition of 64 bits in shared memory is a loop.  A slice has
-// fewer than 2^16 tokens, so that none of the three sums overflows.)
-template <bool WEIGHTS>
-__device__ void count_bits(const RowSlice& row, CutShared& s, CutShared& first, int rank, uint32_t prefix, int shift, uint32_t over, double most) {
+// Counts, by the BITS bits above `shift`, the tokens whose keys have the upper bits `prefix` and are above `over`.  All into the first
+// block's shared memory.
+template <int BITS>
+__device__ void count_bits(const RowSlice& row, CutShared& s, CutShared& first, int rank, uint32_t prefix, int shift, uint32_t over) {
     const int tid = threadIdx.x;
     if (rank != 0) {
-        for (int i = tid; i < 256; i += kRowThreads) { s.sub_n[i] = 0u; s.part[0][i] = s.part[1][i] = s.part[2][i] = 0u; }
+        for (int i = tid; i < 1 << BITS; i += kRowThreads) s.sub_n[i] = 0u;
         __syncthreads();
     }
-    const double edge = value_of<FSD_F32>(prefix << (shift + 8) | ((1u << (shift + 8)) - 1u));
+    for (int i = tid; i < row.n; i += kRowThreads) {
+        const uint4 v = row.vecs[i];
+        const uint32_t bits[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t k = key_of<FSD_F32>(bits[e]);
+            if (k > over && bits[e] != 0xff800000u && k >> (shift + BITS) == prefix) atomicAdd(&s.sub_n[k >> shift & ((1u << BITS) - 1u)], 1u);
+        }
+    }
+    __syncthreads();
+    if (rank != 0)
+        for (int i = tid; i < 1 << BITS; i += kRowThreads)
+            if (s.sub_n[i] != 0u) atomicAdd(&first.sub_n[i], s.sub_n[i]);
+}
+// What a bin's weights are of: nothing in the bin is above it.  In the bin of the largest value that value, so that it weighs 1 without rounding
+// and shares of equal tokens end where they should.
+__device__ __forceinline__ double edge_of(uint32_t prefix, double most) {
+    const double edge = value_of<FSD_F32>(prefix << 16 | 0xffffu);
+    return edge < most ? edge : most;
+}
+// The same by the 7 bits above 9, and what the tokens weigh against the bin's edge, in whole numbers of 1 / kFixed (which a double from 1/4 to 1
+// is: a bin's values are at most 1 apart, but for those below -256, which weigh nothing); and what all tokens above and below the prefix weigh against `most`.
+// (Weights are added by their digits to the base 2^16: an addition of 64 bits in shared memory is a loop.  A slice has
+// fewer than 2^16 tokens, so that none of the four sums overflows.)
+__device__ void weigh_bits(const RowSlice& row, CutShared& s, CutShared& first, int rank, uint32_t prefix, uint32_t over, double most) {
+    const int tid = threadIdx.x;
+    if (rank != 0) {
+        for (int i = tid; i < 512; i += kRowThreads) { s.sub_n[i] = 0u; s.digits[i] = 0u; }
+        __syncthreads();
+    }
+    const double edge = edge_of(prefix, most);
     CountAndWeight above = {0, 0.0}, rest = {0, 0.0};
     for (int i = tid; i < row.n; i += kRowThreads) {
         const uint4 v = row.vecs[i];
         const uint32_t bits[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const uint32_t k = key_of<FSD_F32>(bits[e]), high = k >> (shift + 8);
+            const uint32_t k = key_of<FSD_F32>(bits[e]), high = k >> 16;
             if (k <= over || bits[e] == 0xff800000u) continue;
-            if (!WEIGHTS) {
-                if (high == prefix) atomicAdd(&s.sub_n[k >> shift & 255u], 1u);
-                continue;
-            }
             const double w = exp_of(static_cast<double>(__uint_as_float(bits[e])) - (high == prefix ? edge : most));
             if (high > prefix) above.w += w;
             if (high < prefix) rest.w += w;
             if (high == prefix) {
-                const uint32_t bin = k >> shift & 255u;
+                const uint32_t bin = k >> 9 & 127u;
                 const unsigned long long fixed = __double2ull_rn(w * kFixed);
                 atomicAdd(&s.sub_n[bin], 1u);
-                atomicAdd(&s.part[0][bin], static_cast<uint32_t>(fixed) & 0xffffu);
-                atomicAdd(&s.part[1][bin], static_cast<uint32_t>(fixed >> 16) & 0xffffu);
-                atomicAdd(&s.part[2][bin], static_cast<uint32_t>(fixed >> 32));
+                atomicAdd(&s.digits[bin], static_cast<uint32_t>(fixed) & 0xffffu);
+                atomicAdd(&s.digits[1 * 128 + bin], static_cast<uint32_t>(fixed) >> 16);
+                atomicAdd(&s.digits[2 * 128 + bin], static_cast<uint32_t>(fixed >> 32) & 0xffffu);
+                atomicAdd(&s.digits[3 * 128 + bin], static_cast<uint32_t>(fixed >> 48));
             }
         }
     }
-    if (WEIGHTS) {
-        above = block_total(above, s.scratch);
-        rest = block_total(rest, s.scratch);
-        if (tid == 0) { first.above[rank] = above.w; first.rest[rank] = rest.w; }
-    }
+    above = block_total(above, s.scratch);
+    rest = block_total(rest, s.scratch);
+    if (tid == 0) { first.above[rank] = above.w; first.rest[rank] = rest.w; }
     __syncthreads();
-    for (int i = tid; i < 256; i += kRowThreads) {
-        if (WEIGHTS) {
-            const unsigned long long w = s.part[0][i] + (static_cast<unsigned long long>(s.part[1][i]) << 16) + (static_cast<unsigned long long>(s.part[2][i]) << 32);
-            if (w != 0ull) atomicAdd(reinterpret_cast<unsigned long long*>(&first.sub_w[i]), w);
-        }
-        if (rank != 0 && s.sub_n[i] != 0u) atomicAdd(&first.sub_n[i], s.sub_n[i]);
+    for (int i = tid; i < 128; i += kRowThreads) {
+        if (s.sub_n[i] == 0u) continue;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            atomicAdd(reinterpret_cast<unsigned long long*>(&first.sub_w[h * 128 + i]), s.digits[h * 256 + i] + (static_cast<unsigned long long>(s.digits[h * 256 + 128 + i]) << 16));
+        if (rank != 0) atomicAdd(&first.sub_n[i], s.sub_n[i]);
     }
 }
 
@@ -103,7 +126,8 @@ __device__ __forceinline__ CutResult tell_result(CutShared& s, cg::cluster_group
         const int tid = threadIdx.x;
         __syncthreads();
         if (tid < blocks) *cluster.map_shared_rank(&s.told[turn], tid) = s.work;
-        for (int i = tid; i < 256; i += kRowThreads) { s.sub_n[i] = 0u; s.part[0][i] = s.part[1][i] = s.part[2][i] = 0u; s.sub_w[i] = 0u; }
+        for (int i = tid; i < 512; i += kRowThreads) { s.sub_n[i] = 0u; s.digits[i] = 0u; }
+        for (int i = tid; i < 256; i += kRowThreads) s.sub_w[i] = 0u;
     }
     cluster_barrier();
     return s.told[turn];
@@ -138,7 +162,7 @@ __device__ CutResult refine(const RowSlice& row, const uint32_t* hist, CutShared
     int p_bin = rank == 0 ? s.found[3] : 0;                 // (the first block's) the bin that may have the border of top-p
     if (cut_k) {
         for (int shift = 8; shift >= 0; shift -= 8) {
-            count_bits<false>(row, s, first, rank, res.key, shift, 0u, most);
+            count_bits<8>(row, s, first, rank, res.key, shift, 0u);
             cluster_barrier();
             if (rank == 0) {
                 Run all;
@@ -175,19 +199,19 @@ __device__ CutResult refine(const RowSlice& row, const uint32_t* hist, CutShared
     int last_move = 0;
     while (res.kind == kCutRefineP) {
         const uint32_t prefix = res.key;
-        count_bits<true>(row, s, first, rank, prefix, 8, over, most);
+        weigh_bits(row, s, first, rank, prefix, over, most);
         cluster_barrier();
         if (rank == 0) {
             double above = 0.0, rest = 0.0;
             for (int k = 0; k < blocks; ++k) { above += s.above[k]; rest += s.rest[k]; }
-            const double unit = exp_of(static_cast<double>(value_of<FSD_F32>(prefix << 16 | 0xffffu)) - most) / kFixed;
+            const double unit = exp_of(edge_of(prefix, most) - most) / kFixed;
             Run all;
-            const int bin = 255 - tid;
-            const double w = tid < 256 ? static_cast<double>(s.sub_w[bin]) * unit : 0.0;
-            const uint32_t n = tid < 256 ? s.sub_n[bin] : 0u;
+            const int bin = 127 - tid;
+            const double w = tid < 128 ? __fma_rn(static_cast<double>(s.sub_w[128 + bin]), 4294967296.0, static_cast<double>(s.sub_w[bin])) * unit : 0.0;
+            const uint32_t n = tid < 128 ? s.sub_n[bin] : 0u;
             const Run before = scan_threads({n, w}, s, all);
             const double goal = static_cast<double>(c.top_p) * (above + all.w + rest + of_ties);
-            if (tid == 0) { s.found[1] = -1; s.found[2] = 256; }
+            if (tid == 0) { s.found[1] = -1; s.found[2] = 128; }
             __syncthreads();
             if (n != 0) {
                 atomicMax(&s.found[1], tid);                                      // the last sub-bin in use
@@ -195,7 +219,7 @@ __device__ CutResult refine(const RowSlice& row, const uint32_t* hist, CutShared
             }
             __syncthreads();
             int place = s.found[2];
-            bool up = goal > 0.0 && above >= goal, down = !up && place == 256;
+            bool up = goal > 0.0 && above >= goal, down = !up && place == 128;
             if (down && s.found[1] >= 0 && last_move > 0) { place = s.found[1]; down = false; }
             if (up && s.found[1] >= 0 && last_move < 0) up = false;               // (place is its first sub-bin in use)
             if (down && cut_k && prefix <= over >> 16) {                          // the border is among the tokens equal to the k-th
@@ -211,8 +235,8 @@ __device__ CutResult refine(const RowSlice& row, const uint32_t* hist, CutShared
                     else s.work.key = bin_prefix<FSD_F32>(s, p_bin);
                 }
             } else if (tid == place) {
-                s.work.key = prefix << 8 | static_cast<uint32_t>(bin);
-                s.work.kind = kCutRefineK;                                        // (the last 8 bits)
+                s.work.key = prefix << 7 | static_cast<uint32_t>(bin);
+                s.work.kind = kCutRefineK;                                        // (the last 9 bits)
                 s.goal = goal;
                 s.above_goal = above + before.w;
             }
@@ -221,16 +245,16 @@ __device__ CutResult refine(const RowSlice& row, const uint32_t* hist, CutShared
     }
     if (res.kind == kCutRefineK) {
         const uint32_t prefix = res.key;
-        count_bits<false>(row, s, first, rank, prefix, 0, over, most);
+        count_bits<9>(row, s, first, rank, prefix, 0, over);
         cluster_barrier();
         if (rank == 0) {
             Run all;
-            const int bin = 255 - tid;
-            const uint32_t key = prefix << 8 | static_cast<uint32_t>(bin);
-            const uint32_t n = tid < 256 ? s.sub_n[bin] : 0u;
+            const int bin = 511 - tid;                                            // (a thread each)
+            const uint32_t key = prefix << 9 | static_cast<uint32_t>(bin);
+            const uint32_t n = s.sub_n[bin];
             const double w = n != 0 ? exp_of(static_cast<double>(value_of<FSD_F32>(key)) - most) : 0.0;
             const Run before = scan_threads({n, static_cast<double>(n) * w}, s, all);
-            if (tid == 0) s.found[2] = 256;
+            if (tid == 0) s.found[2] = 512;
             __syncthreads();
             // (where rounding leaves the last of them short of the goal it is the border all the same)
             if (n != 0 && (s.above_goal + before.w + static_cast<double>(n) * w >= s.goal || before.n + n == all.n)) atomicMin(&s.found[2], tid);

@@ -59,7 +59,7 @@ def test_values_next_to_zero_weigh_what_they_weigh(top_k, dtype):
         assert got[:2] == [104821, 28162]
 
 
-@pytest.mark.parametrize("dtype", ["bf16"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n", [100, 1000, 8192, 40000])
 def test_shares_of_equal_tokens_that_end_on_a_token(n, dtype):
     """Of n equal tokens a share of k / n in 32 bits' fractions keeps k: the predecessors of the next one have the share, not less."""
@@ -68,7 +68,7 @@ def test_shares_of_equal_tokens_that_end_on_a_token(n, dtype):
         assert _kept([[(v, n)] for v in values], dtype, [p] * len(values)) == [int(p * n)] * len(values)
 
 
-@pytest.mark.parametrize("dtype", ["bf16"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_shares_of_equal_tokens_in_front_of_others(dtype):
     values = [0.0625, 0.125, -7.8125, -5.875, -3.125, 1.25, 7.5, 12.0]
     # some that top_k leaves out, some below all bins, some that weigh e^-40 of the others
@@ -76,3 +76,11 @@ def test_shares_of_equal_tokens_in_front_of_others(dtype):
     assert _kept([[(v, 1000), (v - 1.0, 5000)] for v in values], dtype, [0.75] * 8, [100] * 8) == [75] * 8
     assert _kept([[(v, 1000), (-30000.0, 5000)] for v in values], dtype, [0.75] * 8) == [750] * 8
     assert _kept([[(v, 1000), (v - 40.0, 50)] for v in values], dtype, [0.75] * 8) == [750] * 8
+
+
+@pytest.mark.parametrize("n", [1000, 30000])
+def test_fp32_a_token_behind_equal_ones_that_weighs_next_to_nothing(n):
+    """What it adds to the share is n * 5e-14 of a token or more, which double precision tells from nothing and 42 bits do not."""
+    values = [1.0, 1.25, 2.5, 3.4375, 0.0625, -3.125]
+    rows = [[(v, n), (v - 25.0 + np.log(n / 1000), 4)] for v in values]
+    assert _kept(rows, "f32", [0.5] * len(values)) == [n // 2 + 1] * len(values)
