@@ -353,7 +353,8 @@ void fsd_default_process_opts(fsd_process_opts *opts);
  * The logits, masks and arrays as in the verify calls: row-major, contiguous, element-aligned; V at most 2^30.  The call is one
  * kernel, or two (biases together with top_k, top_p or min_p; rows that do not fit on chip).  It needs no workspace, and can be captured
  * in a CUDA graph after one ordinary call on that device with the same logit type and with top_k, top_p or min_p set if the captured one has
- * any: that one sets kernels' attributes and copies a table of 64 KB that they read to the device (and waits for that copy alone).
+ * any: that one sets kernels' attributes and copies a table of 64 KB that they read to the device, on a stream of its own, and waits for that
+ * copy alone (CUDA, which loads a kernel at its first use unless CUDA_MODULE_LOADING says otherwise, waits for the device then).
  * Calls share nothing but that table, which stays as it is; outputs do not depend on the order in which a kernel's threads run.
  * Errors: FSD_ERR_NULL (a required pointer, or one of a group that goes together), FSD_ERR_SHAPE, FSD_ERR_ALIGN,
  * FSD_ERR_ENUM, FSD_ERR_UNSUPPORTED (an output overlaps an input that it is not the same as, or another output), FSD_ERR_CUDA. */

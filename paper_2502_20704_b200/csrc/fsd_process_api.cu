@@ -104,6 +104,22 @@ bool rows_shape(const ProcArgs& a, bool raw, RowsShape* shape, size_t* smem) {
     return true;
 }
 
+// The table that the kernels read, by a stream of its own: one that waits for nothing else, and that is waited for, so that the table is there
+// for whatever stream comes next.  (A copy without a stream waits for all blocking streams, and from pageable memory it may return
+// before it is done.)  Another thread's capture, or one of this thread's, goes on undisturbed.
+bool copy_weights(const double (&weights)[kBins]) {
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    if (cudaThreadExchangeStreamCaptureMode(&mode) != cudaSuccess) return false;
+    cudaStream_t own = nullptr;
+    bool ok = cudaStreamCreateWithFlags(&own, cudaStreamNonBlocking) == cudaSuccess;
+    if (ok) {
+        ok = cudaMemcpyToSymbolAsync(bin_weights, weights, sizeof weights, 0, cudaMemcpyHostToDevice, own) == cudaSuccess;
+        ok = cudaStreamSynchronize(own) == cudaSuccess && ok;
+        ok = cudaStreamDestroy(own) == cudaSuccess && ok;
+    }
+    return cudaThreadExchangeStreamCaptureMode(&mode) == cudaSuccess && ok;
+}
+
 // Once a device: the kernels' attributes, and the table they read.
 int prepare_cut() {
     constexpr int kDevices = 64;
@@ -119,7 +135,7 @@ int prepare_cut() {
         cudaFuncSetAttribute(fsd_cut_rows_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kCutSmem)) != cudaSuccess)
         return FSD_ERR_CUDA;
     fill_bin_weights(weights);
-    if (cudaMemcpyToSymbol(bin_weights, weights, sizeof weights) != cudaSuccess) return FSD_ERR_CUDA;
+    if (!copy_weights(weights)) return FSD_ERR_CUDA;
     ready[dev] = true;
     return FSD_OK;
 }
