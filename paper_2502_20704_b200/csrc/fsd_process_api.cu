@@ -140,20 +140,30 @@ int prepare_cut() {
     return FSD_OK;
 }
 
-// Rows that are cut off.  fp32: a cluster of blocks holds a row in shared memory where it fits, else a block sweeps over it in memory.
+// What a launch of the cut needs and could be refused for: in front of a call's first launch, so that a refused call has done nothing.
 template <int DT>
-int launch_cut(const ProcArgs& a, bool raw, cudaStream_t s) {
-    const int rc = prepare_cut();
-    if (rc != FSD_OK) return rc;
+int check_cut(const ProcArgs& a, bool raw) {
     const long long rows = static_cast<long long>(a.B) * (a.rows[0] + a.rows[1]);
     if constexpr (DT == FSD_BF16) {
         RowsShape shape;
         size_t smem;
         if (!rows_shape(a, raw, &shape, &smem)) return FSD_ERR_SHAPE;
+    } else if (const CutShape c = cut_shape(a, raw); c.fits && rows * c.blocks > INT_MAX) {
+        return FSD_ERR_SHAPE;
+    }
+    return prepare_cut();
+}
+// Rows that are cut off.  fp32: a cluster of blocks holds a row in shared memory where it fits, else a block sweeps over it in memory.
+template <int DT>
+int launch_cut(const ProcArgs& a, bool raw, cudaStream_t s) {
+    const long long rows = static_cast<long long>(a.B) * (a.rows[0] + a.rows[1]);
+    if constexpr (DT == FSD_BF16) {
+        RowsShape shape;
+        size_t smem;
+        rows_shape(a, raw, &shape, &smem);
         return put(regular(a, 2) ? fsd_cut_rows_kernel<true> : fsd_cut_rows_kernel<false>, rows, kRowThreads, smem, s, 0, a, shape, raw);
     } else {
         const CutShape c = cut_shape(a, raw);
-        if (rows * c.blocks > INT_MAX) return FSD_ERR_SHAPE;
         if (!c.fits) return put(fsd_cut_long_kernel<DT>, rows, kLongThreads, 0, s, 0, a);
         return put(fsd_cut_cluster_kernel, rows * c.blocks, kRowThreads, c.smem, s, c.blocks, a, c.slice, raw);
     }
@@ -166,7 +176,7 @@ int launch(const ProcArgs& a, bool cut, cudaStream_t s) {
     RowsShape shape;
     size_t smem;
     const bool room = DT == FSD_BF16 ? rows_shape(a, false, &shape, &smem) : cut_shape(a, false).fits;
-    if (cut && a.bias_offsets == nullptr && room) return launch_cut<DT>(a, false, s);
+    const bool one = cut && a.bias_offsets == nullptr && room;
     // a row's vectors, wherever it starts, by blocks
     const long long spans = (a.V + 2 * (Logit<DT>::kPerVec - 1)) / Logit<DT>::kPerVec / kProcThreads + 1;
     // as many rows a block as leave eight blocks an SM, and four at least: what a block sets up is for all of them
@@ -174,7 +184,12 @@ int launch(const ProcArgs& a, bool cut, cudaStream_t s) {
     group = group < 4 ? 4 : group;
     group = group > all ? all : group;
     const long long groups = (all + group - 1) / group;
-    if (spans * groups * a.B > INT_MAX) return FSD_ERR_SHAPE;
+    if (!one && spans * groups * a.B > INT_MAX) return FSD_ERR_SHAPE;
+    if (cut) {
+        const int rc = check_cut<DT>(a, !one);
+        if (rc != FSD_OK) return rc;
+        if (one) return launch_cut<DT>(a, false, s);
+    }
     const int rc = put(regular(a, sizeof(typename Logit<DT>::elem)) ? fsd_process_kernel<DT, true> : fsd_process_kernel<DT, false>, spans * groups * a.B, kProcThreads, 0, s, 0,
                        a, static_cast<int>(spans), static_cast<int>(groups), static_cast<int>(group));
     if (rc != FSD_OK) return rc;

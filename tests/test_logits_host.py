@@ -148,3 +148,12 @@ def test_oracle_history_by_hand():
     assert [int(w) for w in seen[0]] == [0b10, 1 << 8 | 1 << 1] and [int(w) for w in seen[1]] == [1, 0]
     c2, s2 = lo.append(counts, seen, [[1, -1, 2], [41]])
     assert c2[0, 1] == 3 and c2[0, 2] == 1 and int(s2[0, 0]) == 0b110 and np.array_equal(c2[1], counts[1])
+
+
+# ---- calls that are refused have done nothing ------------------------------------------------------
+def test_a_cut_that_cannot_be_launched_is_refused_in_front_of_the_first_kernel():
+    """Biases and a cut are two kernels; fp32 rows by eight blocks each are more blocks than a launch may have.  (Where the first kernel
+    went ahead this gave FSD_ERR_CUDA without a GPU.)"""
+    far = 1 << 50
+    o = fsd.make_process_opts(dtype="f32", bias_offsets=A, bias_tokens=A * 64, bias_values=A * 128, top_p=A * 192)
+    assert _chain(o, t=far, d=far * 2, to=far * 3, do=far * 4, tok=None, B=1 << 20, g=128, V=140000) == binding.FSD_ERR_SHAPE
