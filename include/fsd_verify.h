@@ -357,7 +357,8 @@ void fsd_default_process_opts(fsd_process_opts *opts);
  * copy alone (CUDA, which loads a kernel at its first use unless CUDA_MODULE_LOADING says otherwise, waits for the device then).
  * Calls share nothing but that table, which stays as it is; outputs do not depend on the order in which a kernel's threads run.
  * Errors: FSD_ERR_NULL (a required pointer, or one of a group that goes together), FSD_ERR_SHAPE, FSD_ERR_ALIGN,
- * FSD_ERR_ENUM, FSD_ERR_UNSUPPORTED (an output overlaps an input that it is not the same as, or another output), FSD_ERR_CUDA. */
+ * FSD_ERR_ENUM, FSD_ERR_UNSUPPORTED (an output overlaps another output, or an input; a side's own logits may be the same; the two lists of
+ * biases, whose lengths the host does not know, are not looked at), FSD_ERR_CUDA. */
 int fsd_process_chain(const void *target_in, const void *draft_in, const int32_t *draft_tokens,
                       int B, int gamma, int V, const fsd_process_opts *opts,
                       void *target_out, void *draft_out, void *stream);

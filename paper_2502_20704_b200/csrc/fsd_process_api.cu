@@ -209,10 +209,11 @@ int process(const void* target_in, const void* draft_in, const int32_t* parent, 
         {target_in, nt}, {draft_in, nd}, {parent, nB * P}, {tokens, nB * P}, {o->counts, nB * V}, {o->seen, B * W4}, {o->repetition, nB}, {o->frequency, nB},
         {o->presence, nB}, {o->bias_offsets, nB + 4}, {o->allowed, static_cast<size_t>(B) * (P + 1) * W4}, {o->temperature, nB}, {o->top_k, nB}, {o->top_p, nB},
         {o->min_p, nB}};
+    // (a side's own input may be its output, and nothing else that happens to start there)
     for (const auto& in : ins) {
         if (in.p == nullptr) continue;
-        if (overlap(in.p, in.n, target_out, nt) && !(in.p == target_in && target_in == target_out)) return FSD_ERR_UNSUPPORTED;
-        if (nd != 0 && overlap(in.p, in.n, draft_out, nd) && !(in.p == draft_in && draft_in == draft_out)) return FSD_ERR_UNSUPPORTED;
+        if (overlap(in.p, in.n, target_out, nt) && !(&in == &ins[0] && target_in == target_out)) return FSD_ERR_UNSUPPORTED;
+        if (nd != 0 && overlap(in.p, in.n, draft_out, nd) && !(&in == &ins[1] && draft_in == draft_out)) return FSD_ERR_UNSUPPORTED;
     }
     if (overlap(target_out, nt, draft_out, nd)) return FSD_ERR_UNSUPPORTED;
     ProcArgs a = {};

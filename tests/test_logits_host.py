@@ -157,3 +157,17 @@ def test_a_cut_that_cannot_be_launched_is_refused_in_front_of_the_first_kernel()
     far = 1 << 50
     o = fsd.make_process_opts(dtype="f32", bias_offsets=A, bias_tokens=A * 64, bias_values=A * 128, top_p=A * 192)
     assert _chain(o, t=far, d=far * 2, to=far * 3, do=far * 4, tok=None, B=1 << 20, g=128, V=140000) == binding.FSD_ERR_SHAPE
+
+
+def test_an_output_that_is_another_input_of_the_same_address_is_refused():
+    o = fsd.make_process_opts(dtype="f32", repetition=A, temperature=A * 2)
+    plain = fsd.make_process_opts(dtype="f32")
+    assert _chain(plain, t=A, to=A, d=A) == binding.FSD_ERR_UNSUPPORTED          # the draft's rows are read from what becomes the target's
+    assert _chain(plain, t=A, d=A, do=A) == binding.FSD_ERR_UNSUPPORTED
+    assert _chain(plain, t=A, to=A, tok=A) == binding.FSD_ERR_UNSUPPORTED
+    assert _chain(plain, d=A * 2, do=A * 2, tok=A * 2) == binding.FSD_ERR_UNSUPPORTED
+    assert _chain(o, t=A, to=A) == binding.FSD_ERR_UNSUPPORTED
+    assert _chain(o, d=A * 2, do=A * 2, t=A * 9) == binding.FSD_ERR_UNSUPPORTED
+    tree = lambda t, d, par, to, do: fsd.fsd_process_tree(t, d, par, None, 2, 3, 64, plain, to, do, None)  # noqa: E731
+    assert tree(A, A * 2, A, A, A * 5) == binding.FSD_ERR_UNSUPPORTED
+    assert tree(A, A, A * 9, A, A * 5) == binding.FSD_ERR_UNSUPPORTED
