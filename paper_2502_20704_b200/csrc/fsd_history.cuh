@@ -10,7 +10,8 @@ constexpr int kHistSpan = 11264;        // ids a block counts, in shared memory
 
 // A block per sequence and span of the vocabulary.  It looks through all of the sequence's tokens, which the L2 cache has after
 // the first block, so that nothing has to be cleared first and each count is written once.  Whole numbers: the order of
-// the additions does not matter.  32 sequences of up to 32768 + 8192 tokens, V = 128256: 11 us, of which the longest sequence's
+// the additions does not matter.  (Places in the lists are counted in 64 bits: an offset may be 2^31 - 1, and a thread's next place
+// behind it.)  32 sequences of up to 32768 + 8192 tokens, V = 128256: 11 us, of which the longest sequence's
 // tokens are most; the counts alone are 2.6 us of memory.
 __global__ void __launch_bounds__(kHistThreads) fsd_history_build_kernel(const int32_t* prompt_offsets, const int32_t* prompt_tokens, const int32_t* output_offsets,
                                                                          const int32_t* output_tokens, int V, int W, int spans, int32_t* counts, uint32_t* seen) {
@@ -21,13 +22,13 @@ __global__ void __launch_bounds__(kHistThreads) fsd_history_build_kernel(const i
     for (int i = threadIdx.x; i < kHistSpan / 32; i += kHistThreads) bits[i] = 0u;
     __syncthreads();
 #pragma unroll 8
-    for (int i = __ldg(prompt_offsets + b) + static_cast<int>(threadIdx.x), end = __ldg(prompt_offsets + b + 1); i < end; i += kHistThreads) {
+    for (long long i = __ldg(prompt_offsets + b) + static_cast<long long>(threadIdx.x), end = __ldg(prompt_offsets + b + 1); i < end; i += kHistThreads) {
         const int t = __ldg(prompt_tokens + i), k = t - lo;
         if (t >= lo && t < V && k < kHistSpan) atomicOr(&bits[k >> 5], 1u << (k & 31));
     }
     if (output_offsets != nullptr)
 #pragma unroll 8
-        for (int i = __ldg(output_offsets + b) + static_cast<int>(threadIdx.x), end = __ldg(output_offsets + b + 1); i < end; i += kHistThreads) {
+        for (long long i = __ldg(output_offsets + b) + static_cast<long long>(threadIdx.x), end = __ldg(output_offsets + b + 1); i < end; i += kHistThreads) {
             const int t = __ldg(output_tokens + i), k = t - lo;
             if (t >= lo && t < V && k < kHistSpan) {
                 atomicAdd(&n[k], 1);
@@ -46,12 +47,12 @@ __global__ void __launch_bounds__(128) fsd_history_append_kernel(const int32_t* 
     if (b >= B) return;
     int n = __ldg(accept_len + b);
     n = n < 0 ? 0 : n > width ? width : n;
-    for (int i = lane; i <= n; i += 32) {
+    for (long long i = lane; i <= n; i += 32) {              // (n may be 2^31 - 1)
         int t;
         if (i == n) {
             t = __ldg(next_token + b);
         } else {
-            const int j = path != nullptr ? __ldg(path + static_cast<size_t>(b) * width + i) : i;
+            const int j = path != nullptr ? __ldg(path + static_cast<size_t>(b) * width + i) : static_cast<int>(i);
             t = j >= 0 && j < P ? __ldg(tokens + static_cast<size_t>(b) * P + j) : -1;
         }
         if (t >= 0 && t < V) {

@@ -104,10 +104,10 @@ __device__ __forceinline__ void find_sparse(const ProcArgs& a, int b, int lo, Sp
     if (a.bias_offsets != nullptr)
         for (int i = threadIdx.x; i < SPAN; i += blockDim.x) s.bias[i] = 0;
     __syncthreads();
-    for (int i = b0 + static_cast<int>(threadIdx.x); i < b1; i += blockDim.x) {
+    for (long long i = b0 + static_cast<long long>(threadIdx.x); i < b1; i += blockDim.x) {               // (an offset may be 2^31 - 1)
         const int t = __ldg(a.bias_tokens + i), k = t - lo;
         if (t >= 0 && t < a.V && k >= 0 && k < SPAN) {
-            atomicMax(&s.bias[k], i - b0 + 1);
+            atomicMax(&s.bias[k], static_cast<int>(i - b0) + 1);
             atomicOr(&s.drafted[k >> 5], 1u << (k & 31));
         }
     }
