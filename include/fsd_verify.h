@@ -308,8 +308,8 @@ int fsd_accept_labels(const float *divergence, int B, int positions, float thres
  *   x    = used ? (x > 0 ? x * (1 / repetition[b]) : x * repetition[b]) : x
  *   x    = x - frequency[b] * n,  then  x = x - presence[b] if n > 0
  *   x    = x + bias of t
- *   x    = -inf if bit t of the row's mask is 0, whatever the logit is
  *   x    = x * (1 / temperature[b]) if temperature[b] > 0
+ *   x    = -inf if bit t of the row's mask is 0, whatever the logit and the settings are
  *   y    = x, rounded to the logits' type
  * in single precision, each operation (1 / repetition and 1 / temperature are two of them) rounded to nearest by itself.
  * With any of top_k, top_p and min_p set, the row y is then cut off.  In the order of falling value, equal values by rising

@@ -72,13 +72,14 @@ def process_row(x, counts=None, seen=None, drafted=(), repetition=None, frequenc
     for t, v in last.items():
         x[t] += v
         size[t] += abs(v)
+    if temperature is not None and temperature > 0:
+        with np.errstate(invalid="ignore"):
+            x = x / float(np.float32(temperature))
+            size = size / float(np.float32(temperature))
     if allowed is not None:
         for t in range(V):
             if not bit(allowed, t):
                 x[t] = -np.inf
-    if temperature is not None and temperature > 0:
-        x = x / float(np.float32(temperature))
-        size = size / float(np.float32(temperature))
     return x, size
 
 

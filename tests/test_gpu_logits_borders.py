@@ -1,4 +1,5 @@
-"""Borders of top-p that are decided by little: rows in which one weight or its rounding says where the cut is."""
+"""Borders of top-p that are decided by little: rows in which one weight or its rounding says where the cut is.  And settings at
+the ends of their ranges."""
 
 import numpy as np
 import pytest
@@ -84,3 +85,37 @@ def test_fp32_a_token_behind_equal_ones_that_weighs_next_to_nothing(n):
     values = [1.0, 1.25, 2.5, 3.4375, 0.0625, -3.125]
     rows = [[(v, n), (v - 25.0 + np.log(n / 1000), 4)] for v in values]
     assert _kept(rows, "f32", [0.5] * len(values)) == [n // 2 + 1] * len(values)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("steps", [("mask", "temp"), ("pen", "bias", "mask", "temp"), ("pen", "mask", "temp", "k", "p", "m"), ("pen", "bias", "mask", "temp", "k", "p", "m")])
+def test_masked_tokens_stay_masked_at_any_temperature(steps, dtype):
+    """1 / temperature is 0 or infinite at the ends, and its product with -inf or 0 no number."""
+    c = lg.Call(4, 2, 1003, dtype, steps, seed=41)
+    c.o["temperature"] = np.array([np.inf, 3.4028235e38, 1e-38, 0.5], np.float32)
+    got = c.run()
+    whole = c.run(c.opts(top_k=None, top_p=None, min_p=None))
+    for side, x in whole.items():
+        for b in range(4):
+            for r in range(x.shape[1]):
+                row = lo.context_row(None, side, r)
+                off = torch.tensor([not lo.bit(c.o["allowed"][b, row], t) for t in range(c.V)])
+                assert (x[b, r][off] == -float("inf")).all() and (got[side][b, r][off] == -float("inf")).all(), (side, b, r)
+                assert b != 0 or (x[b, r][~off] == 0).all()
+    if "k" in steps:
+        c.check_cut(got, whole)
+    # A value whose magnitude is 2^128 (1 - 2^-25) or more rounds to infinity in single precision (and in bf16), which the oracle's doubles do not:
+    # with a temperature of 1e-38 these are the logits from 3.4 on.  The rest is held to the usual tolerance.  (2^-20 beside the border covers
+    # the eight roundings of 2^-24 on the way.)  1 / 3.4e38 is subnormal and off by 2^-150 at most, so |x| times it by |x| 2^-150, less than the 8 * 2^-24 of it that
+    # are granted (|x| 1.1 * 2^-149), and the product by TINY.
+    far = 2.0 ** 128
+    for side, x in whole.items():
+        for b in range(4):
+            for r in range(x.shape[1]):
+                y = x[b, r].double().numpy()
+                want, size = c.want(side, b, r)
+                over = np.abs(want) > far * (1 + 2.0 ** -20)
+                assert np.array_equal(y[over], np.sign(want[over]) * np.inf)
+                fin = np.abs(want) < far * (1 - (2.0 ** -20 if dtype == "f32" else 2.0 ** -7))
+                may = 8 * 2.0 ** -24 * size[fin] + lg.HALF_STEP[dtype] * (np.abs(want[fin]) + 8 * 2.0 ** -24 * size[fin]) + lg.TINY[dtype]
+                assert (np.abs(y[fin] - want[fin]) <= may).all(), (side, b, r)

@@ -171,3 +171,8 @@ def test_an_output_that_is_another_input_of_the_same_address_is_refused():
     tree = lambda t, d, par, to, do: fsd.fsd_process_tree(t, d, par, None, 2, 3, 64, plain, to, do, None)  # noqa: E731
     assert tree(A, A * 2, A, A, A * 5) == binding.FSD_ERR_UNSUPPORTED
     assert tree(A, A, A * 9, A, A * 5) == binding.FSD_ERR_UNSUPPORTED
+
+
+def test_oracle_masks_hold_at_any_temperature():
+    y, _ = lo.process_row([1.0, -math.inf, 2.0, -math.inf], allowed=np.array([0b0011], np.uint32), temperature=math.inf)
+    assert y[0] == 0.0 and math.isnan(y[1]) and y[2:].tolist() == [-math.inf, -math.inf]
