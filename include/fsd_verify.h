@@ -258,6 +258,12 @@ int fsd_set_group_size(int group_size);
  * shape.  The word is zero after a call in which no check failed. */
 int fsd_debug_checks(int B, int positions, size_t *word_offset);
 
+/* The same for the calls that have no workspace (fsd_process_*, fsd_history_*): their kernels' checks -- places in the lists of sparse
+ * ids, token ids, 16-byte accesses, bins and slices -- go into one int of the library's on each device.  Stores it in *word (host pointer; the
+ * current device's; what is on a non-blocking stream has to be waited for first); 0 in the release build.
+ * Errors: FSD_ERR_NULL, FSD_ERR_CUDA. */
+int fsd_debug_process_word(int *word);
+
 /* ---- Threshold tuning (Section "Selecting T"; Discussion, "Potential further developments") ----
  * The paper tunes T on a small development set by running FSD at candidate thresholds and
  * looking at the speed each gives, and notes that FSD's decisions are a deterministic function

@@ -104,6 +104,8 @@ def _load():
         lib.fsd_calibrate_threshold.restype = C.c_int
         lib.fsd_accept_labels.argtypes = [vp, C.c_int, C.c_int, C.c_float, C.c_int, vp, C.c_void_p]
         lib.fsd_accept_labels.restype = C.c_int
+        lib.fsd_debug_process_word.argtypes = [C.POINTER(C.c_int)]
+        lib.fsd_debug_process_word.restype = C.c_int
         lib.fsd_default_process_opts.argtypes = [C.POINTER(FsdProcessOpts)]
         lib.fsd_default_process_opts.restype = None
         lib.fsd_process_chain.argtypes = [vp, vp, ip, C.c_int, C.c_int, C.c_int, C.POINTER(FsdProcessOpts), vp, vp, vp]
@@ -250,6 +252,15 @@ def fsd_calibrate_threshold(divergence, B, positions, target_mean_accept_len, co
 
 def fsd_accept_labels(divergence, B, positions, threshold, compare, labels, stream=None) -> int:
     return _load().fsd_accept_labels(_ptr(divergence), B, positions, float(threshold), compare, _ptr(labels), stream)
+
+
+def fsd_debug_process_word() -> int:
+    """What range checks have failed in the calls without a workspace: 0, and always 0 unless the library is the debug build."""
+    word = C.c_int(0)
+    rc = _load().fsd_debug_process_word(C.byref(word))
+    if rc != 0:
+        raise FsdError(rc)
+    return word.value
 
 
 def fsd_default_process_opts() -> FsdProcessOpts:

@@ -11,7 +11,7 @@
 // Index and range checks of the debug build (-DFSD_DEBUG_CHECKS, see build.py): a failed check
 // sets a bit in the workspace's debug word and the access goes ahead as in the release build --
 // the checks are there to show that it never happens, on inputs of every shape the tests run.
-// `word` points to the debug word of the workspace's block of flags.
+// `word` points to the debug word of the workspace's block of flags, or (calls without a workspace) to one of the library's own.
 #ifdef FSD_DEBUG_CHECKS
 #define FSD_CHECK(word, cond, code) do { if (!(cond)) atomicOr((word), (code)); } while (0)
 #else
@@ -24,7 +24,7 @@ namespace cg = cooperative_groups;
 
 // bits of the debug word
 constexpr int kChkItem = 1, kChkSlice = 2, kChkStage = 4, kChkTmem = 8, kChkRecord = 16, kChkRow = 32, kChkChunk = 64,
-              kChkToken = 128, kChkPath = 256;
+              kChkToken = 128, kChkPath = 256, kChkVector = 512, kChkList = 1024, kChkBin = 2048;
 
 // The workspace's block of flags.  A verify call is known by a number of its own: what its messages between thread
 // blocks and its timeout flag carry, so that nothing the workspace held before is taken for this call's and

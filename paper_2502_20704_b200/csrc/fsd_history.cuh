@@ -36,6 +36,7 @@ __global__ void __launch_bounds__(kHistThreads) fsd_history_build_kernel(const i
             }
         }
     __syncthreads();
+    FSD_CHECK(&process_debug, lo >= 0 && lo < V && lo % 32 == 0, kChkSlice);
     for (int k = threadIdx.x; k < kHistSpan && lo + k < V; k += kHistThreads) counts[static_cast<size_t>(b) * V + lo + k] = n[k];
     for (int k = threadIdx.x; k < kHistSpan / 32 && lo / 32 + k < W; k += kHistThreads) seen[static_cast<size_t>(b) * W + lo / 32 + k] = bits[k];
 }

@@ -128,6 +128,7 @@ __device__ __forceinline__ void find_sparse(const ProcArgs& a, int b, int lo, Sp
         int at = atomicAdd(&s.n, __popc(any));
         for (uint32_t todo = any; todo != 0u; todo &= todo - 1u) {
             const int e = __ffs(static_cast<int>(todo)) - 1;
+            FSD_CHECK(&process_debug, at >= 0 && at < SPAN && t + e < a.V, kChkList);
             s.counts[at] = (used >> e & 1u) ? __ldg(a.counts + static_cast<size_t>(b) * a.V + t + e) : -1;
             s.list[at++] = static_cast<uint16_t>(k + e);
         }
@@ -139,6 +140,7 @@ __device__ __forceinline__ void find_sparse(const ProcArgs& a, int b, int lo, Sp
 template <int DT>
 __device__ __forceinline__ uint4 load_ids(const void* row, int t0, int V, bool whole) {
     constexpr int N = Logit<DT>::kPerVec;
+    FSD_CHECK(&process_debug, !whole || (t0 >= 0 && t0 + N <= V && reinterpret_cast<uintptr_t>(static_cast<const typename Logit<DT>::elem*>(row) + t0) % 16 == 0), kChkVector);
     if (whole) return *reinterpret_cast<const uint4*>(static_cast<const typename Logit<DT>::elem*>(row) + t0);
     uint32_t w[4];
 #pragma unroll
@@ -176,6 +178,7 @@ __device__ __forceinline__ uint4 pack_vec(const float (&x)[Logit<DT>::kPerVec]) 
 }
 template <int DT>
 __device__ __forceinline__ void store_ids(void* row, int t0, int V, bool whole, const uint4& v) {
+    FSD_CHECK(&process_debug, !whole || (t0 >= 0 && t0 + Logit<DT>::kPerVec <= V && reinterpret_cast<uintptr_t>(static_cast<typename Logit<DT>::elem*>(row) + t0) % 16 == 0), kChkVector);
     if (whole) {
         *reinterpret_cast<uint4*>(static_cast<typename Logit<DT>::elem*>(row) + t0) = v;
     } else {
@@ -263,6 +266,7 @@ __global__ void __launch_bounds__(kProcThreads) fsd_process_kernel(const ProcArg
     const uint32_t settings[4] = {__float_as_uint(a.repetition != nullptr ? __ldg(a.repetition + b) : 1.f), __float_as_uint(a.frequency != nullptr ? __ldg(a.frequency + b) : 0.f),
                                   __float_as_uint(a.presence != nullptr ? __ldg(a.presence + b) : 0.f), __float_as_uint(a.temperature != nullptr ? __ldg(a.temperature + b) : 0.f)};
     const SeqParams p = seq_params(settings);
+    FSD_CHECK(&process_debug, b < a.B && n_sparse <= kSpan, kChkItem);
     const int all = a.rows[0] + a.rows[1], first = group * group_rows, last = first + group_rows < all ? first + group_rows : all;
 
     const uint32_t* allowed = a.allowed != nullptr ? a.allowed + static_cast<size_t>(b) * (a.P + 1) * a.W : nullptr;
@@ -318,6 +322,7 @@ __global__ void __launch_bounds__(kProcThreads) fsd_process_kernel(const ProcArg
     const int stride = kProcThreads / wide;
     for (int k = static_cast<int>(threadIdx.x) % wide; k < n_sparse; k += wide) {
         const int at = sparse.list[k], t = lo + at, count = sparse.counts[k];
+        FSD_CHECK(&process_debug, at < kSpan && t >= 0 && t < a.V, kChkToken);
         const bool again = sparse.drafted[at >> 5] >> (at & 31) & 1u;
         const int entry = again && a.bias_offsets != nullptr ? sparse.bias[at] : 0;
         const float bias = entry > 0 ? __ldg(a.bias_values + __ldg(a.bias_offsets + b) + entry - 1) : 0.f;

@@ -7,6 +7,11 @@
 
 #include "fsd_verify.h"
 #include "fsd_device.cuh"
+#ifdef FSD_DEBUG_CHECKS
+namespace fsd {
+static __device__ int process_debug;       // what range checks of this file's kernels have failed
+}
+#endif
 #include "fsd_history.cuh"
 #include "fsd_process.cuh"
 #include "fsd_truncate.cuh"
@@ -269,6 +274,15 @@ int fsd_process_tree(const void* target_in, const void* draft_in, const int32_t*
     if (parent == nullptr) return FSD_ERR_NULL;
     if (N < 1 || N > kMaxNodes) return FSD_ERR_SHAPE;
     return process(target_in, draft_in, parent, node_tokens, B, N, V, opts, target_out, draft_out, stream);
+}
+
+int fsd_debug_process_word(int* word) {
+    if (word == nullptr) return FSD_ERR_NULL;
+    *word = 0;
+#ifdef FSD_DEBUG_CHECKS
+    if (cudaMemcpyFromSymbol(word, process_debug, sizeof *word) != cudaSuccess) return FSD_ERR_CUDA;
+#endif
+    return FSD_OK;
 }
 
 int fsd_history_build(const int32_t* prompt_offsets, const int32_t* prompt_tokens, const int32_t* output_offsets, const int32_t* output_tokens,

@@ -324,6 +324,7 @@ __device__ __noinline__ void count_value(uint32_t bits, uint32_t* hist, BinsShar
         if (key < *reinterpret_cast<volatile uint32_t*>(&s->under_lo)) atomicMin(&s->under_lo, key);
         if (key > *reinterpret_cast<volatile uint32_t*>(&s->under_hi)) atomicMax(&s->under_hi, key);
     }
+    FSD_CHECK(&process_debug, bin >= 0 && bin < kBins, kChkBin);
     atomicAdd(&hist[bin], static_cast<uint32_t>(BY));
 }
 __device__ __forceinline__ uint32_t min_halves(uint32_t a, uint32_t b) {
@@ -370,6 +371,8 @@ __device__ __forceinline__ void count_vec(const uint4& v, uint32_t* hist, BinsSh
             uint32_t* mid = hist + kHalfBins;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
+                FSD_CHECK(&process_debug, static_cast<int16_t>(bin[k]) >= -kHalfBins && static_cast<int16_t>(bin[k]) < kHalfBins && (static_cast<int>(bin[k]) >> 16) >= -kHalfBins &&
+                                              (static_cast<int>(bin[k]) >> 16) < kHalfBins, kChkBin);
                 atomicAdd(mid + static_cast<int16_t>(bin[k]), 1u);
                 atomicAdd(mid + (static_cast<int>(bin[k]) >> 16), 1u);
             }
@@ -380,7 +383,11 @@ __device__ __forceinline__ void count_vec(const uint4& v, uint32_t* hist, BinsSh
         for (int e = 0; e < 4; ++e) {
             const uint32_t mag = bits[e] >> 16 & 0x7fffu;
             if (mag <= kMagLo || mag >= kMagHi) count_value<DT, 1>(bits[e], hist, s);
-            else atomicAdd(&hist[static_cast<int>((mag - kMagLo) ^ static_cast<uint32_t>(static_cast<int>(bits[e]) >> 31)) + kHalfBins], 1u);
+            else {
+                const int bin = static_cast<int>((mag - kMagLo) ^ static_cast<uint32_t>(static_cast<int>(bits[e]) >> 31)) + kHalfBins;
+                FSD_CHECK(&process_debug, bin >= 0 && bin < kBins, kChkBin);
+                atomicAdd(&hist[bin], 1u);
+            }
         }
     }
 }
@@ -583,6 +590,7 @@ __device__ __forceinline__ void solve_bins(const uint32_t* hist, BinsShared& s, 
         }
     }
     const int p_bin = kBins - 1 - p_place;
+    FSD_CHECK(&process_debug, !(cut_k || c.p) || (p_place >= 0 && p_place <= kBins && k_place >= -1 && k_place < kBins && top_bin >= 0), kChkBin);
     if (c.p && (p_bin < 0 || !one_value(s, p_bin) || !sure)) {
         __syncthreads();
         if (tid == 0) s.work.kind = kCutByBits;

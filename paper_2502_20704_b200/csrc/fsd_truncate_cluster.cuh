@@ -286,6 +286,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_cluster_kernel(const P
     const int blocks = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
     const int all = a.rows[0] + a.rows[1], line = blockIdx.x / blocks, b = line / all, q = line % all;
     const int side = q >= a.rows[0], r = q - (side ? a.rows[0] : 0);
+    FSD_CHECK(&process_debug, b < a.B && r < a.rows[side] && blocks <= kMaxCutCluster && slice * N <= 65536, kChkItem);
     const size_t at = (static_cast<size_t>(b) * a.rows[side] + r) * a.V;
     const elem* in = static_cast<const elem*>(raw ? a.out[side] : a.in[side]) + at;
     elem* out = static_cast<elem*>(a.out[side]) + at;
@@ -319,6 +320,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_cluster_kernel(const P
     const uint32_t* allowed = !raw && a.allowed != nullptr ? a.allowed + (static_cast<size_t>(b) * (a.P + 1) + ctx) * a.W : nullptr;
     const int ids_lo = row.first > 0 ? row.first : 0, ids_hi = row.first + row.n * N < a.V ? row.first + row.n * N : a.V;   // of the slice
     const int word0 = ids_lo >> 5, n_words = ids_hi > ids_lo ? ((ids_hi + 31) >> 5) - word0 : 0;
+    FSD_CHECK(&process_debug, row.n <= slice && n_words <= slice * N / 32 + 2, kChkSlice);
     clear_bins(hist, s);
     if (drafts > 0)
         for (int i = tid; i < n_words; i += kRowThreads) drafted_ids[i] = 0u;
@@ -327,6 +329,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_cluster_kernel(const P
     cluster_arrive();                                       // from here on others may add to the first block's counts
     for (int j = tid; j < drafts; j += kRowThreads) {
         const int t = __ldg(a.tokens + static_cast<size_t>(b) * a.P + j);
+        FSD_CHECK(&process_debug, t < ids_lo || t >= ids_hi || ((t >> 5) - word0 >= 0 && (t >> 5) - word0 < n_words), kChkList);
         if (t >= ids_lo && t < ids_hi) atomicOr(&drafted_ids[(t >> 5) - word0], 1u << (t & 31));
     }
     const CutParams c = cut_params(s.settings, a.V);
@@ -387,6 +390,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_cluster_kernel(const P
             at -= __popc(todo);
             for (int base = 0; base < total; base += kListed) {
                 while (todo != 0u && at < base + kListed) {
+                    FSD_CHECK(&process_debug, at >= base && lane * 32 + 31 < 65536, kChkList);
                     s.list[warp][at - base] = static_cast<uint16_t>(lane * 32 + __ffs(static_cast<int>(todo)) - 1);
                     todo &= todo - 1u;
                     ++at;
@@ -400,6 +404,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_cluster_kernel(const P
                     const uint32_t is_draft = __shfl_sync(0xffffffffu, draft, l >> 5) >> (l & 31) & 1u;
                     if (k >= n) continue;
                     const int t = (word0 + w0 + (l >> 5) * kRowWarps) * 32 + (l & 31);
+                    FSD_CHECK(&process_debug, t >= ids_lo && t < ids_hi && t - row.first >= 0 && t - row.first < row.n * N, kChkToken);
                     const int count = is_used ? __ldg(a.counts + static_cast<size_t>(b) * a.V + t) : -1;
                     const float x = read_id<DT>(in, t);
                     const int d = is_draft ? drafted(a, b, ctx, t) : 0;

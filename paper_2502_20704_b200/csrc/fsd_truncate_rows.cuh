@@ -59,6 +59,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const Proc
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int all = a.rows[0] + a.rows[1], b = blockIdx.x / all, q = blockIdx.x % all;
     const int side = q >= a.rows[0], r = q - (side ? a.rows[0] : 0);
+    FSD_CHECK(&process_debug, b < a.B && r < a.rows[side], kChkItem);
     const size_t at = (static_cast<size_t>(b) * a.rows[side] + r) * a.V;
     const uint16_t* in = static_cast<const uint16_t*>(raw ? a.out[side] : a.in[side]) + at;
     uint16_t* out = static_cast<uint16_t*>(a.out[side]) + at;
@@ -126,6 +127,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const Proc
             const auto add = [&](int j) {
                 const int t = __ldg(a.tokens + static_cast<size_t>(b) * a.P + j);
                 if (t < 0 || t >= a.V || !(allowed == nullptr || (__ldg(allowed + (t >> 5)) >> (t & 31) & 1u))) return;
+                FSD_CHECK(&process_debug, t >> 5 < shape.words, kChkList);
                 atomicOr(&bitmap[t >> 5], 1u << (t & 31));
                 atomicOr(&s.some[t >> 5 & 7], 1u << (t & 31));
             };
@@ -148,6 +150,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const Proc
                 const uint32_t used = history ? __ldg(seen + w) : 0u;
                 for (uint32_t todo = bitmap[w]; todo != 0u; todo &= todo - 1u) {
                     const int e = __ffs(static_cast<int>(todo)) - 1;
+                    FSD_CHECK(&process_debug, n < static_cast<uint32_t>(shape.cap) && w * 32 + e < a.V, kChkList);
                     list[n++] = static_cast<uint32_t>(w * 32 + e) | (used >> e & 1u) << 31;
                 }
             }
@@ -161,7 +164,9 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const Proc
             const int e = __ffs(static_cast<int>(todo)) - 1, t = t0 + e;
             todo &= todo - 1u;
             uint32_t half;
+            FSD_CHECK(&process_debug, t >= 0 && t < a.V, kChkToken);
             if (listed) {
+                FSD_CHECK(&process_debug, ahead[t >> 5] + __popc(bitmap[t >> 5] & ((1u << (t & 31)) - 1u)) < n_sparse, kChkList);
                 half = list[ahead[t >> 5] + __popc(bitmap[t >> 5] & ((1u << (t & 31)) - 1u))];
             } else {
                 const bool used = history && (__ldg(seen + (t >> 5)) >> (t & 31) & 1u);
@@ -177,6 +182,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const Proc
         for (int k = tid; k < n_sparse; k += kRowThreads) {
             const uint32_t entry = list[k];                 // (its highest bit: the id is used)
             const int t = static_cast<int>(entry & 0x7fffffffu), count = (entry >> 31) != 0u ? __ldg(a.counts + static_cast<size_t>(b) * a.V + t) : -1;
+            FSD_CHECK(&process_debug, t < a.V, kChkToken);
             const float x = read_id<DT>(in, t);
             const uint32_t is = pack_bf16(value_of_id(t, x, count), 0.f) & 0xffffu;
             list[k] = is;
