@@ -104,10 +104,11 @@ __device__ __forceinline__ void find_sparse(const ProcArgs& a, int b, int lo, Sp
     if (a.bias_offsets != nullptr)
         for (int i = threadIdx.x; i < SPAN; i += blockDim.x) s.bias[i] = 0;
     __syncthreads();
-    for (long long i = b0 + static_cast<long long>(threadIdx.x); i < b1; i += blockDim.x) {               // (an offset may be 2^31 - 1)
-        const int t = __ldg(a.bias_tokens + i), k = t - lo;
+    const int biases = b1 > b0 ? b1 - b0 : 0;
+    for (int left = biases - static_cast<int>(threadIdx.x); left > 0; left -= static_cast<int>(blockDim.x)) {      // (counted down: an offset may be 2^31 - 1)
+        const int t = __ldg(a.bias_tokens + b0 + (biases - left)), k = t - lo;
         if (t >= 0 && t < a.V && k >= 0 && k < SPAN) {
-            atomicMax(&s.bias[k], static_cast<int>(i - b0) + 1);
+            atomicMax(&s.bias[k], biases - left + 1);
             atomicOr(&s.drafted[k >> 5], 1u << (k & 31));
         }
     }
