@@ -208,8 +208,12 @@ __global__ void __launch_bounds__(kRowThreads, 2) fsd_cut_rows_kernel(const Proc
     CutResult res = {kCutNone, 0u, a.V, 0u};
     if (cutting) {
         // Of a row that keeps few tokens, two tiles say what is below the last of them: vectors of such values alone are passed over.
-        // (Not where sparse ids are not listed: they may become more than they were.)
-        const bool few = c.k && c.top_k <= kTile && n_vecs >= 8 * kTile && (n_sparse == 0 || listed);
+        // (Not where sparse ids are not listed: they may become more than they were.)  A row of V = 8 n_vecs tokens gains while what the two
+        // tiles say leaves few vectors to look at, us without / with it for 1088 rows:
+        //   V = 152064: top_k 1 224 / 195, 20 231 / 212, 50 236 / 230, 64 237 / 237, 100 241 / 247, 1000 258 / 275
+        //   V = 98304: 20 152 / 142, 32 155 / 151, 50 157 / 157      V = 65536: 10 109 / 103, 20 110 / 108, 32 111 / 113
+        //   V = 49152: 20 90.7 / 91.7    V = 32768: 20 68 / 75
+        const bool few = c.k && c.top_k <= n_vecs / 320 && n_vecs >= 8 * kTile && (n_sparse == 0 || listed);
         const bool leaving_out = listed || allowed != nullptr;
         bool passing = false;
         __nv_bfloat162 from = __bfloat162bfloat162(__float2bfloat16_rn(0.f));
