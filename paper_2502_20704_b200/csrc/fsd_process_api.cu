@@ -72,7 +72,13 @@ bool regular(const ProcArgs& a, size_t es) {
     return is;
 }
 
-// fp32: how a row lies in the shared memory of a cluster's blocks.
+// fp32: how a row lies in the shared memory of a cluster's blocks: at most 4096 vectors a block, and 2048 where there are fewer blocks than two
+// an SM.  us with top-p 0.9 by clusters of 1 / 2 / 4 / 8 blocks (- does not fit), what the rule takes in brackets:
+//   1 x 8192: 25.6 / [23.4] / 21.6 / 19.5         1 x 32000: 50 / 36 / [25.6] / 22.6      1 x 128256: - / - / 50 / [35.6]
+//   32 x 8192: 25.3 / [23.3] / 22.3 / 23.8        32 x 32000: 71 / 48 / [35.6] / 33.7     32 x 128256: - / - / 52 / [52]
+//   148 x 8192: 33.6 / [35.8] / 69 / 102          148 x 32000: 71 / [56] / 83 / 118       148 x 128256: - / - / 253 / [229]
+//   1088 x 8192: [126] / 194 / 349 / 652          1088 x 16384: 200 / [257] / 407 / 747   1088 x 32000: 394 / [349] / 485 / 796
+// It is not always the fastest: a row or two go faster in more blocks (1 x 32000 in eight, by 3 us), and many rows of 16384 in one.
 struct CutShape {
     int blocks, slice;         // slice: vectors a block has
     size_t smem;
