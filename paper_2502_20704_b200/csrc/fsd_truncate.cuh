@@ -66,11 +66,11 @@ __device__ __forceinline__ long long ties_below(double above, double w, double g
 // (Out of line: the places that need it are many and reached seldom.)
 __device__ __noinline__ double exp_d(double x) { return exp(x); }
 
-// exp(x) for x of at most 700, to a few units of the last place: x = n ln 2 + r with |r| <= ln 2 / 2, and e^r by its
+// exp(x) for x of at most 700, to 2^-52 of itself (0.61 of that at most over 750000 values): x = n ln 2 + r with |r| <= ln 2 / 2, and e^r by its
 // Taylor series up to r^13 / 13! (the next term is below 5e-18).  Sums that say where a border lies need that much of each of
 // their terms.  Below -700 it is 0.
 __device__ __forceinline__ double exp_of(double x) {
-    if (!(x > -700.0)) return 0.0;
+    if (!(x >= -700.0)) return 0.0;
     const double shift = 6755399441055744.0;                                      // 1.5 * 2^52: adding it rounds to a whole number
     const double u = __fma_rn(x, kLog2eD, shift);
     const int n = __double2loint(u);
