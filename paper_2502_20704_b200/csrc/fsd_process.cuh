@@ -93,6 +93,8 @@ template <int SPAN> struct Sparse {
     int n;
 };
 // All of the block's threads.  lo: the span's first id, a multiple of 32 (it may be negative).  Ends with a barrier.
+// Each block reads all of the sequence's list of biases, which is for lists of a few thousand: 64 x 17 x 152064 takes 124 us with 16 a sequence, 142 with
+// 300, 176 with 3000 and 1099 with one for every token; 1 x 152064 6.9, 6.8, 8.8 and 59.
 template <int SPAN>
 __device__ __forceinline__ void find_sparse(const ProcArgs& a, int b, int lo, Sparse<SPAN>& s) {
     static_assert(SPAN % 32 == 0, "whole words");

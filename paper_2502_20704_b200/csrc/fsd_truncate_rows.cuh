@@ -7,7 +7,7 @@ namespace fsd {
 
 // The block reads the row twice and keeps none of it: once to count its values, and again, from the L2 cache for the most part
 // (two blocks an SM have 90 MB of rows of 152064 on the way), to write it.  No block waits for another, which is what most of
-// a cluster's time went into: 64 x 17 x 152064 took 660 us that way and takes 273 (top_p; 352 with penalties and mixed settings).
+// a cluster's time went into: 64 x 17 x 152064 took 660 us that way and takes 268 (top_p; 347 to 360 with penalties and mixed settings).
 // What bounds it now is its instructions, some 300 for 8 logits: 8 additions to the bins and their addresses, the mask, the temperature
 // and the border once or twice.
 // Sparse ids, which the count of the others leaves out, are listed in front: a bitmap of the row's, the sum of its bits up to each word, and for
