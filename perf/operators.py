@@ -358,9 +358,12 @@ def _own(s):
             _ok(fsd, fsd.fsd_history_append_chain(s["tokens"], s["accept_len"], s["next_token"], B, P, V, s["counts"], s["seen"], s["stream"]))
         return {"counts": s["counts"], "seen": s["seen"]}
     if "opts" not in s:         # a program makes the options once, with the buffers they point to
-        s["opts"] = fsd.make_process_opts(
-            dtype=case["dtype"], **{k: s[k] for k in ("counts", "seen", "repetition", "frequency", "presence", "bias_offsets", "bias_tokens",
-                                                      "bias_values", "allowed", "temperature", "top_k", "top_p", "min_p")})
+        arrays = {k: s[k] for k in ("counts", "seen", "repetition", "frequency", "presence", "bias_offsets", "bias_tokens", "bias_values", "allowed",
+                                    "temperature", "top_k", "top_p", "min_p")}
+        if s["bias_offsets"] is not None:       # of a token listed twice the call takes the last entry: both say what they add up to
+            at = s["bias_tokens"].view(B, -1).long()
+            arrays["bias_values"] = torch.zeros(B, V, device=at.device).scatter_add_(1, at, s["bias_values"].view(B, -1)).gather(1, at).view(-1)
+        s["opts"] = fsd.make_process_opts(dtype=case["dtype"], **arrays)
     if case["call"] == "tree":
         _ok(fsd, fsd.fsd_process_tree(s["target"], s["draft"], s["parent"], s["tokens"], B, P, V, s["opts"], s["target_out"], s["draft_out"],
                                       s["stream"]))
